@@ -313,6 +313,93 @@ int32_t ceca_graph_rounds(const float* X_in, float* X_out, int32_t n, int64_t d,
                           const int32_t* nbr, const float* w, const float* w_self, int32_t m,
                           int32_t period, int32_t k0, int32_t rounds, void* hip_stream);
 
+/* ---- Operators of language models whose parameters are the agents' rows ----
+ * The two ends of a language model between which the caller's own layers stand: the lookup of token embeddings in every
+ * agent's row and its gradient, written where the gradient rows of CECA_LOSS_GRADIENT lie; the loss against a teacher's top
+ * logits with its gradient; and a row's top logits, which an agent sends its peers in place of all its logits.
+ * Activations and logits are fp32, bf16 or fp16; parameters, gradients of parameters and losses are fp32.  Everything is
+ * computed in fp32 and rounded once, to nearest even, where a result is stored in 16 bits.  The results of a call depend on
+ * its arguments alone: no floating-point atomics are used.  Pointers lie on their element type's boundary (CECA_EINVAL
+ * otherwise); pitches are counted in elements.  n T, the number of positions, is below 2^31; T = 0 does nothing (and
+ * ceca_embed_grad then sees no token). */
+enum { CECA_F32 = 0, CECA_BF16 = 1, CECA_F16 = 2 };
+
+/* Embedding lookup: out row i T + t = scale * row tokens[i T + t] of agent i's table, i < n, t < T.
+ * E: device, agent i's table is V rows of h floats, ldr apart, from E + i lde on -- a part of row i of a state, say.
+ * tokens: device, n T int32; one outside [0, V) stands for padding: a row of zeros.
+ * out: device, n T rows of h elements of `type`, ldo apart; disjoint from E and tokens.
+ * Needs h <= ldr <= 2^31 - 1, h <= ldo, and lde >= (V - 1) ldr + h with more than one agent. */
+int32_t ceca_embed(const float* E, int64_t lde, int64_t ldr, int32_t n, int32_t V, int32_t h, const int32_t* tokens, int32_t T,
+                   float scale, void* out, int32_t type, int64_t ldo, void* hip_stream);
+
+/* Bytes of device workspace ceca_embed_grad needs; < 0 on error. */
+int64_t ceca_embed_grad_workspace_bytes(int32_t n, int32_t V, int32_t h, int32_t T);
+
+/* Gradient of ceca_embed with respect to the tables:
+ *   row v of agent i's part of E  (+)=  scale * sum over the t with tokens[i T + t] = v of G's row i T + t,
+ * E laid out as above, G as out.  accumulate = 0 writes every row of every table, zeros where a token does not occur (the
+ * contents of E are not read); otherwise the sums are added and rows of tokens that do not occur are left alone -- tables that
+ * serve as output layer too, several microbatches.  Tokens outside [0, V) contribute nothing and G's rows there are not read.
+ * What lies between rows (ldr > h) and tables is left alone.  E is disjoint from G and tokens.
+ * workspace: device, 256-byte aligned, at least ceca_embed_grad_workspace_bytes(); its contents are scratch. */
+int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t* tokens, int32_t T, float scale, int32_t accumulate,
+                        float* E, int64_t lde, int64_t ldr, int32_t n, int32_t V, int32_t h,
+                        void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits.  For every position (row i T + t) with student logits s (V of them) and the K
+ * entries (u_k, id_k) of its teacher,
+ *   p = softmax(u / temperature) over the entries,  q = softmax(s / temperature),  r = softmax(s):
+ *   loss = weight [ (1 - hard) temperature^2 sum_k p_k (log p_k - log q_id_k)  +  hard (-log r_label) ]
+ *   gradient by s_v = weight [ (1 - hard) temperature (q_v - sum_{k: id_k = v} p_k)  +  hard (r_v - [v = label]) ]
+ * The teacher's row is the position's own or, with `peer`, position t of agent peer[i] (ceca_schedule's map, say): agents
+ * that teach each other read each other's entries in place.
+ *   - An id outside [0, V) or a value of -inf is no entry.  An id that comes twice counts twice.
+ *   - A row without entries has no soft term, one whose label is outside [0, V) no hard term; K = 0 with labels and hard > 0
+ *     is the plain cross entropy.
+ *   - A logit of -inf is masked: q_v = r_v = 0.  An entry or label there has an infinite loss and the formula's gradient.
+ *     The type's lowest finite value is an ordinary logit.
+ *   - A row with neither term, or with every logit -inf, has loss 0 and a zero gradient.  So has one of weight 0, whose logits
+ *     and entries are not looked at (padding may hold anything).
+ *   - A NaN or +inf among a row's logits makes its loss and its whole gradient NaN; one among its entries' values its soft
+ *     loss and the gradient at its entries' places. */
+#define CECA_TOP_MAX 256
+typedef struct {
+  int32_t n, T, V;
+  int32_t K;               /* entries per position, 0 .. CECA_TOP_MAX */
+  int32_t type;            /* of the logits and of the gradient */
+  float temperature;       /* 0.001 .. 1000 */
+  float hard;              /* share of the hard term, 0 .. 1; needs labels when not 0 */
+  const void* logits;      /* device, n T rows of V elements */
+  int64_t ld;              /* >= V */
+  const float* top;        /* device, n T K: the teacher's logits, in any order */
+  const int32_t* ids;      /* device, n T K: their places */
+  const int32_t* peer;     /* device, n, or NULL; values outside [0, n) are clamped into it */
+  const int32_t* labels;   /* device, n T, or NULL */
+  const float* weight;     /* device, n T, or NULL (ones): the factor of the row's loss in the whole loss */
+} ceca_distill_t;
+
+/* Bytes of device workspace ceca_distill needs for this problem (may be 0); < 0 on error. */
+int64_t ceca_distill_workspace_bytes(const ceca_distill_t* spec);
+
+/* Loss (device, n T floats, or NULL) and gradient (device, n T rows of V elements of the logits' type, ldg apart, or NULL) in
+ * one call; at least one of them.  A training loop that learns the weights later (autograd) asks for the loss first and calls
+ * again for the gradient, with the weights it was handed.  The gradient may overwrite the logits (grad = logits, ldg = ld) or
+ * is disjoint from all inputs; the loss is disjoint from everything.  Columns of a row past V are left alone.
+ * workspace: device, 256-byte aligned, at least ceca_distill_workspace_bytes() (may be NULL when that is 0); scratch. */
+int32_t ceca_distill(const ceca_distill_t* spec, float* loss, void* grad, int64_t ldg, void* workspace, int64_t workspace_bytes,
+                     void* hip_stream);
+
+/* Bytes of device workspace ceca_top_logits needs (may be 0); < 0 on error. */
+int64_t ceca_top_logits_workspace_bytes(int32_t type, int32_t rows, int32_t V, int32_t K);
+
+/* The K largest (1 .. CECA_TOP_MAX) of every row's V logits, from the largest down, the lower place first among equals
+ * (-0 equals +0; NaN counts above +inf): top (device, rows K floats) and ids (device, rows K int32).  Logits of -inf are
+ * masked: where fewer than K others are there, -inf and the place -1 fill up, which ceca_distill takes as no entry.
+ * logits: device, `rows` rows of V elements of `type`, ld apart; top and ids are disjoint from it and from each other.
+ * workspace: device, 256-byte aligned, at least ceca_top_logits_workspace_bytes() (may be NULL when that is 0); scratch. */
+int32_t ceca_top_logits(const void* logits, int32_t type, int64_t ld, int32_t rows, int32_t V, int32_t K, float* top, int32_t* ids,
+                        void* workspace, int64_t workspace_bytes, void* hip_stream);
+
 /* Message for the calling thread's most recent error ("" if none); valid until its next failing call. */
 const char* ceca_last_error(void);
 /* hipError_t value behind the calling thread's most recent CECA_EHIP (0 if none). */

@@ -15,12 +15,16 @@ OPT_SEGMENT, OPT_ROWS, OPT_BAND, OPT_WG_PER_CU, OPT_ONEPASS, OPT_AGENTS_PER_WG, 
 OPT_GRAPH_STAGE, OPT_CHUNKED_GRADIENT, OPT_CONS_STRIPS, OPT_PROBE_WAVES, OPT_LEAN_TILES, OPT_PROBE_VARIANT, OPT_HALF_STEP_RUN, OPT_WINDOW_MISSING = 11, 12, 13, 14, 15, 16, 17, 18
 TOPO_RING, TOPO_STATIC_EXP, TOPO_ONE_PEER_EXP = 0, 1, 2
 MIX_MAX = 16
+TOP_MAX = 256
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2            # CECA_F32, CECA_BF16, CECA_F16
 # forms of the minibatch calls, as ceca_last_form (ceca_test.h) names them
 FORM_NONE, FORM_STEP_SINGLE, FORM_STEP_ONE_PASS, FORM_STEP_TWO_PASS, FORM_RUN_WINDOW, FORM_RUN_HALF_STEPS, FORM_RUN_MESSAGES, FORM_RUN_TWO_PASS, FORM_RUN_STEPS = range(9)
 
 EXPORTS = (
     "ceca_tau", "ceca_schedule", "ceca_gossip_round", "ceca_gossip_rounds", "ceca_average", "dsgd_ceca_workspace_bytes", "dsgd_ceca_step", "dsgd_ceca_steps", "dsgd_ceca_run_workspace_bytes", "dsgd_ceca_run",
-    "consensus_error_workspace_bytes", "consensus_error", "consensus_error_noalloc", "ceca_state_consensus", "ceca_topology_round", "ceca_mix_rounds", "ceca_graph_rounds", "ceca_last_error", "ceca_last_hip_error",
+    "consensus_error_workspace_bytes", "consensus_error", "consensus_error_noalloc", "ceca_state_consensus", "ceca_topology_round", "ceca_mix_rounds", "ceca_graph_rounds",
+    "ceca_embed", "ceca_embed_grad_workspace_bytes", "ceca_embed_grad", "ceca_distill_workspace_bytes", "ceca_distill", "ceca_top_logits_workspace_bytes", "ceca_top_logits",
+    "ceca_last_error", "ceca_last_hip_error",
 )
 # include/ceca_test.h: launch-shape overrides and probe kernels for tests and measurement, not the product ABI
 TEST_EXPORTS = ("ceca_set_option", "ceca_reset_options", "ceca_stream_probe", "ceca_describe_step_launch", "ceca_last_form", "ceca_last_window_on_one_xcd")
@@ -49,6 +53,12 @@ class Loss(C.Structure):
 class Mix(C.Structure):
     """ceca_mix_t"""
     _fields_ = [("m", C.c_int32), ("w_self", C.c_float), ("shift", C.c_int32 * MIX_MAX), ("w", C.c_float * MIX_MAX)]
+
+
+class Distill(C.Structure):
+    """ceca_distill_t"""
+    _fields_ = [(k, C.c_int32) for k in ("n", "T", "V", "K", "type")] + [("temperature", C.c_float), ("hard", C.c_float), ("logits", C.c_void_p), ("ld", C.c_int64)] + \
+               [(k, C.c_void_p) for k in ("top", "ids", "peer", "labels", "weight")]
 
 
 _lib = None
@@ -109,6 +119,23 @@ def lib():
         L.ceca_graph_rounds.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p,
                                         C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
         L.ceca_graph_rounds.restype = C.c_int32
+        L.ceca_embed.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_void_p,
+                                 C.c_int32, C.c_int64, C.c_void_p]
+        L.ceca_embed.restype = C.c_int32
+        L.ceca_embed_grad_workspace_bytes.argtypes = [C.c_int32] * 4
+        L.ceca_embed_grad_workspace_bytes.restype = C.c_int64
+        L.ceca_embed_grad.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int32, C.c_float, C.c_int32, C.c_void_p, C.c_int64,
+                                      C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+        L.ceca_embed_grad.restype = C.c_int32
+        L.ceca_distill_workspace_bytes.argtypes = [C.POINTER(Distill)]
+        L.ceca_distill_workspace_bytes.restype = C.c_int64
+        L.ceca_distill.argtypes = [C.POINTER(Distill), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+        L.ceca_distill.restype = C.c_int32
+        L.ceca_top_logits_workspace_bytes.argtypes = [C.c_int32] * 4
+        L.ceca_top_logits_workspace_bytes.restype = C.c_int64
+        L.ceca_top_logits.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_int64, C.c_void_p]
+        L.ceca_top_logits.restype = C.c_int32
         L.ceca_stream_probe.argtypes = [C.c_void_p] * 5 + [C.c_int64, C.c_int32, C.c_int32, C.c_void_p]
         L.ceca_stream_probe.restype = C.c_int32
         L.ceca_describe_step_launch.argtypes = [C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
@@ -232,6 +259,157 @@ def dsgd_ceca_run(S_in, S_out, n: int, d: int, loss: Loss, batch_idx, lr: float,
     wbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().dsgd_ceca_run(_ptr(S_in), _ptr(S_out), n, d, ld, C.byref(loss), _ptr(batch_idx), lr, r0, iters, port,
                                _ptr(workspace), wbytes, _stream(stream)))
+
+
+# ---- operators of language models: tensors come with types and shapes here, so they are checked against the sizes ----
+
+def _refuse(msg: str):
+    raise CecaError(CECA_EINVAL, msg)
+
+
+def _elem_type(name: str, t) -> int:
+    import torch
+    code = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}.get(t.dtype)
+    return _refuse(f"{name} is {t.dtype}: float32, bfloat16 or float16 needed") if code is None else code
+
+
+def _rows_pitch(name: str, t, rows: int, width: int) -> int:
+    """The pitch of a tensor that holds `rows` rows of `width` contiguous elements, whatever its leading dimensions."""
+    if t.dim() < 1 or t.shape[-1] != width or t.numel() != rows * width:
+        _refuse(f"{name} has the shape {tuple(t.shape)}: {rows} rows of {width} needed")
+    if width > 1 and t.stride(-1) != 1:
+        _refuse(f"{name}: the elements of a row have to be contiguous")
+    if rows == 0:
+        return width
+    pitch, inner = None, 1
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size != 1:
+            if pitch is None:
+                pitch = stride
+            elif stride != pitch * inner:
+                _refuse(f"{name}: its rows have to lie at one pitch")
+            inner *= size
+    return width if pitch is None else int(pitch)
+
+
+def _flat(name: str, t, dtype: str, count: int) -> None:
+    if str(t.dtype) != "torch." + dtype or t.numel() != count or not t.is_contiguous():
+        _refuse(f"{name}: {count} contiguous elements of {dtype} needed, not {tuple(t.shape)} of {t.dtype}")
+
+
+def _on_device(stream, *tensors) -> None:
+    """Kernels run on the current device: tensors and stream have to be its own."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            _refuse(f"a tensor on {t.device}: the current device's memory (cuda:{dev}) is needed")
+    if stream is not None and stream.device.index != dev:
+        _refuse(f"a stream of {stream.device}: the current device is cuda:{dev}")
+
+
+def _tables(E, n: int, V: int, h: int):
+    """(lde, ldr) of the agents' tables: E of n rows that begin with V rows of h floats each, or of the shape (n, V, h)."""
+    if str(E.dtype) != "torch.float32":
+        _refuse(f"E is {E.dtype}: float32 needed")
+    if E.dim() == 3 and tuple(E.shape) == (n, V, h) and (h == 1 or E.stride(2) == 1):
+        return int(E.stride(0)), int(E.stride(1)) if V > 1 else max(h, int(E.stride(1)))
+    if E.dim() == 2 and E.shape[0] == n and E.shape[1] >= V * h and (E.shape[1] == 1 or E.stride(1) == 1):
+        return int(E.stride(0)), h
+    return _refuse(f"E has the shape {tuple(E.shape)} and the strides {tuple(E.stride())}: ({n}, {V}, {h}) or {n} rows of at least {V * h} needed, rows contiguous")
+
+
+def _positions(tokens, n: int) -> int:
+    if n < 1 or tokens.numel() % n:
+        _refuse(f"{tokens.numel()} tokens are no whole number for each of n = {n} agents")
+    _flat("tokens", tokens, "int32", tokens.numel())
+    return tokens.numel() // n
+
+
+def _workspace_bytes(workspace) -> int:
+    if workspace is None:
+        return 0
+    if not workspace.is_contiguous():
+        _refuse("workspace has to be contiguous")
+    return workspace.numel() * workspace.element_size()
+
+
+def ceca_embed(E, n: int, V: int, h: int, tokens, out, scale: float = 1.0, stream=None) -> None:
+    """out = scale * the rows of the agents' tables at `tokens`.  E: float32, (n, V, h) or n rows (of a state, say) that begin
+    with the table; tokens: int32, n x T; out: n x T rows of h, float32, bfloat16 or float16."""
+    T = _positions(tokens, n)
+    lde, ldr = _tables(E, n, V, h)
+    ldo = _rows_pitch("out", out, n * T, h)
+    _on_device(stream, E, tokens, out)
+    _check(lib().ceca_embed(_ptr(E), lde, ldr, n, V, h, _ptr(tokens), T, scale, _ptr(out), _elem_type("out", out), ldo, _stream(stream)))
+
+
+def ceca_embed_grad_workspace_bytes(n: int, T: int, V: int, h: int) -> int:
+    return _check(lib().ceca_embed_grad_workspace_bytes(n, V, h, T))
+
+
+def ceca_embed_grad(G, n: int, V: int, h: int, tokens, E, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None) -> None:
+    """The gradient of ceca_embed's tables for the gradient G of its output, written to E (laid out as the tables) or added to it."""
+    T = _positions(tokens, n)
+    lde, ldr = _tables(E, n, V, h)
+    ldg = _rows_pitch("G", G, n * T, h)
+    _on_device(stream, G, tokens, E, workspace)
+    _check(lib().ceca_embed_grad(_ptr(G), _elem_type("G", G), ldg, _ptr(tokens), T, scale, int(accumulate), _ptr(E), lde, ldr, n, V, h,
+                                 _ptr(workspace), _workspace_bytes(workspace), _stream(stream)))
+
+
+def make_distill(logits, n: int, T: int, V: int, top=None, ids=None, peer=None, labels=None, weight=None, temperature: float = 1.0,
+                 hard: float = 0.0) -> Distill:
+    """logits: n x T rows of V, float32, bfloat16 or float16; top, ids: n x T x K float32 and int32, the teacher's entries; peer: n
+    int32, whose entries agent i reads; labels: n x T int32; weight: n x T float32 (all on the device)."""
+    if n < 1 or T < 0 or V < 1:
+        _refuse(f"need n, V >= 1 and T >= 0 (n = {n}, T = {T}, V = {V})")
+    if (top is None) != (ids is None):
+        _refuse("top and ids come together")
+    K = 0
+    if top is not None:
+        K = int(top.shape[-1]) if top.dim() else 0
+        _flat("top", top, "float32", n * T * K)
+        _flat("ids", ids, "int32", n * T * K)
+    for name, t, dtype, count in (("peer", peer, "int32", n), ("labels", labels, "int32", n * T), ("weight", weight, "float32", n * T)):
+        if t is not None:
+            _flat(name, t, dtype, count)
+    spec = Distill(n=n, T=T, V=V, K=K, type=_elem_type("logits", logits), temperature=temperature, hard=hard, logits=_ptr(logits),
+                   ld=_rows_pitch("logits", logits, n * T, V), top=_ptr(top), ids=_ptr(ids), peer=_ptr(peer), labels=_ptr(labels),
+                   weight=_ptr(weight))
+    spec.tensors = (logits, top, ids, peer, labels, weight)
+    return spec
+
+
+def ceca_distill_workspace_bytes(spec: Distill) -> int:
+    return _check(lib().ceca_distill_workspace_bytes(C.byref(spec)))
+
+
+def ceca_distill(spec: Distill, loss=None, grad=None, workspace=None, stream=None) -> None:
+    """loss: n x T float32, or None; grad: n x T rows of V of the logits' type (or the logits themselves), or None."""
+    ldg = 0
+    if loss is not None:
+        _flat("loss", loss, "float32", spec.n * spec.T)
+    if grad is not None:
+        if _elem_type("grad", grad) != spec.type:
+            _refuse(f"grad is {grad.dtype}: the logits' type is needed")
+        ldg = _rows_pitch("grad", grad, spec.n * spec.T, spec.V)
+    _on_device(stream, loss, grad, workspace, *getattr(spec, "tensors", ()))
+    _check(lib().ceca_distill(C.byref(spec), _ptr(loss), _ptr(grad), ldg, _ptr(workspace), _workspace_bytes(workspace), _stream(stream)))
+
+
+def ceca_top_logits_workspace_bytes(logits, rows: int, V: int, K: int) -> int:
+    return _check(lib().ceca_top_logits_workspace_bytes(_elem_type("logits", logits), rows, V, K))
+
+
+def ceca_top_logits(logits, rows: int, V: int, K: int, top, ids, workspace=None, stream=None) -> None:
+    """The K largest logits of every row and their places (top: float32, ids: int32, rows x K), from the largest down."""
+    ld = _rows_pitch("logits", logits, rows, V)
+    _flat("top", top, "float32", rows * K)
+    _flat("ids", ids, "int32", rows * K)
+    _on_device(stream, logits, top, ids, workspace)
+    _check(lib().ceca_top_logits(_ptr(logits), _elem_type("logits", logits), ld, rows, V, K, _ptr(top), _ptr(ids), _ptr(workspace),
+                                 _workspace_bytes(workspace), _stream(stream)))
 
 
 def consensus_error_workspace_bytes(n: int, d: int) -> int:

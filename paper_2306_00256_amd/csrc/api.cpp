@@ -12,6 +12,7 @@
 #include "ceca_test.h"
 #include "launch.h"
 #include "schedule.h"
+#include "text.h"
 
 namespace ceca {
 thread_local Tuning g_tuning{};     // all zero: the library's own launch shapes
@@ -603,6 +604,71 @@ int32_t scratch_of_current_device(char** out) {
     g_scratch_ptr[dev] = p;
   }
   *out = reinterpret_cast<char*>(g_scratch_ptr[dev]);
+  return CECA_OK;
+}
+
+// ---- operators of language models ----
+
+int64_t elem_size(int32_t type) { return type == CECA_F32 ? 4 : 2; }
+bool on_elements(const void* p, int64_t size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) == 0; }
+
+// Bytes from the first to the last element of `rows` rows of `width` elements, `pitch` apart; 0 without rows.
+// (More than 2^47 bytes lie beyond any device's memory; the product must not overflow.)
+constexpr int64_t kMostBytes = 1LL << 47;
+bool span_bytes(int64_t rows, int64_t pitch, int64_t width, int64_t size, int64_t* bytes) {
+  *bytes = 0;
+  if (rows == 0) return true;
+  const __int128 b = ((__int128)(rows - 1) * pitch + width) * size;
+  if (b > kMostBytes) return false;
+  *bytes = (int64_t)b;
+  return true;
+}
+
+int32_t check_tables(const void* E, int64_t lde, int64_t ldr, int32_t n, int32_t V, int32_t h, const void* rows, int32_t type, int64_t ldo,
+                     const void* tokens, int32_t T, int64_t* table_bytes, int64_t* row_bytes) {
+  if (n < 1 || V < 1 || h < 1 || T < 0) return fail(CECA_EINVAL, "need n, V, h >= 1 and T >= 0 (n = %d, V = %d, h = %d, T = %d)", n, V, h, T);
+  if ((int64_t)n * T > INT32_MAX) return fail(CECA_EINVAL, "n T = %lld: need fewer than 2^31 positions", (long long)n * T);
+  if (type < CECA_F32 || type > CECA_F16) return fail(CECA_EINVAL, "unknown element type %d", type);
+  if (!E || (T > 0 && (!rows || !tokens))) return fail(CECA_EINVAL, "null pointer");
+  if (ldr < h || ldr > INT32_MAX || ldo < h)
+    return fail(CECA_EINVAL, "need h <= ldr < 2^31 and h <= the rows' pitch (h = %d, ldr = %lld, pitch = %lld)", h, (long long)ldr, (long long)ldo);
+  const int64_t table = (int64_t)(V - 1) * ldr + h;
+  if (n > 1 && lde < table) return fail(CECA_EINVAL, "lde = %lld: a table takes %lld floats", (long long)lde, (long long)table);
+  if (!on_elements(E, 4) || !on_elements(tokens, 4) || !on_elements(rows, elem_size(type)))
+    return fail(CECA_EINVAL, "pointers must lie on element boundaries");
+  if (!span_bytes(n, lde, table, 4, table_bytes) || !span_bytes((int64_t)n * T, ldo, h, elem_size(type), row_bytes))
+    return fail(CECA_EINVAL, "sizes beyond the address space");
+  return CECA_OK;
+}
+
+int32_t check_workspace(const void* workspace, int64_t have, int64_t need) {
+  if (need == 0) return CECA_OK;
+  if (!workspace || have < need) return fail(CECA_EWORKSPACE, "workspace of %lld bytes needed, %lld given", (long long)need, (long long)(workspace ? have : 0));
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(CECA_EWORKSPACE, "workspace must be 256-byte aligned");
+  return CECA_OK;
+}
+
+int32_t check_distill(const ceca_distill_t* p) {
+  if (!p) return fail(CECA_EINVAL, "null pointer");
+  if (p->n < 1 || p->V < 1 || p->T < 0) return fail(CECA_EINVAL, "need n, V >= 1 and T >= 0 (n = %d, V = %d, T = %d)", p->n, p->V, p->T);
+  if ((int64_t)p->n * p->T > INT32_MAX) return fail(CECA_EINVAL, "n T = %lld: need fewer than 2^31 positions", (long long)p->n * p->T);
+  if (p->type < CECA_F32 || p->type > CECA_F16) return fail(CECA_EINVAL, "unknown element type %d", p->type);
+  if (p->K < 0 || p->K > CECA_TOP_MAX) return fail(CECA_EINVAL, "K = %d outside [0, %d]", p->K, CECA_TOP_MAX);
+  if (!(p->temperature >= 1e-3f && p->temperature <= 1e3f)) return fail(CECA_EINVAL, "temperature %g outside [0.001, 1000]", (double)p->temperature);
+  if (!(p->hard >= 0.0f && p->hard <= 1.0f)) return fail(CECA_EINVAL, "hard = %g outside [0, 1]", (double)p->hard);
+  if (p->ld < p->V) return fail(CECA_EINVAL, "need V <= ld (V = %d, ld = %lld)", p->V, (long long)p->ld);
+  if (p->K == 0 && p->hard == 0.0f) return fail(CECA_EINVAL, "neither entries (K = 0) nor a hard term");
+  if (p->T > 0 && (!p->logits || (p->K > 0 && (!p->top || !p->ids)) || (p->hard > 0.0f && !p->labels))) return fail(CECA_EINVAL, "null pointer");
+  if (!on_elements(p->logits, elem_size(p->type)) || !on_elements(p->top, 4) || !on_elements(p->ids, 4) || !on_elements(p->peer, 4) ||
+      !on_elements(p->labels, 4) || !on_elements(p->weight, 4))
+    return fail(CECA_EINVAL, "pointers must lie on element boundaries");
+  return CECA_OK;
+}
+
+int32_t check_top(int32_t type, int32_t rows, int32_t V, int32_t K) {
+  if (rows < 0 || V < 1) return fail(CECA_EINVAL, "need rows >= 0 and V >= 1 (rows = %d, V = %d)", rows, V);
+  if (type < CECA_F32 || type > CECA_F16) return fail(CECA_EINVAL, "unknown element type %d", type);
+  if (K < 1 || K > CECA_TOP_MAX) return fail(CECA_EINVAL, "K = %d outside [1, %d]", K, CECA_TOP_MAX);
   return CECA_OK;
 }
 
@@ -1325,6 +1391,108 @@ int32_t ceca_graph_rounds(const float* X_in, float* X_out, int32_t n, int64_t d,
   const hipError_t e = ceca::launch_graph_rounds(g, tile.vec4, st);
   if (e != hipSuccess) return hip_fail(e, "graph gossip kernel launch");
   return CECA_OK;
+}
+
+int32_t ceca_embed(const float* E, int64_t lde, int64_t ldr, int32_t n, int32_t V, int32_t h, const int32_t* tokens, int32_t T,
+                   float scale, void* out, int32_t type, int64_t ldo, void* hip_stream) {
+  int64_t tb, rb;
+  const int32_t rc = check_tables(E, lde, ldr, n, V, h, out, type, ldo, tokens, T, &tb, &rb);
+  if (rc != CECA_OK) return rc;
+  if (overlaps(E, tb, out, rb) || overlaps(tokens, (int64_t)n * T * 4, out, rb)) return fail(CECA_EINVAL, "out overlaps an input");
+  if (T == 0) return CECA_OK;
+  ceca::EmbedArgs a{};
+  a.E = E;  a.lde = lde;  a.ldr = ldr;  a.tokens = tokens;  a.rows = out;  a.ldo = ldo;
+  a.n = n;  a.V = V;  a.h = h;  a.T = T;  a.type = type;  a.scale = scale;
+  const hipError_t e = ceca::launch_embed(a, (hipStream_t)hip_stream);
+  return e == hipSuccess ? CECA_OK : hip_fail(e, "embedding kernel launch");
+}
+
+int64_t ceca_embed_grad_workspace_bytes(int32_t n, int32_t V, int32_t h, int32_t T) {
+  if (n < 1 || V < 1 || h < 1 || T < 0 || (int64_t)n * T > INT32_MAX)
+    return fail(CECA_EINVAL, "need n, V, h >= 1, T >= 0 and n T < 2^31 (n = %d, V = %d, h = %d, T = %d)", n, V, h, T);
+  return 0;
+}
+
+int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t* tokens, int32_t T, float scale, int32_t accumulate,
+                        float* E, int64_t lde, int64_t ldr, int32_t n, int32_t V, int32_t h,
+                        void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  int64_t tb, rb;
+  int32_t rc = check_tables(E, lde, ldr, n, V, h, G, type, ldg, tokens, T, &tb, &rb);
+  if (rc != CECA_OK) return rc;
+  const int64_t need = ceca_embed_grad_workspace_bytes(n, V, h, T);
+  rc = check_workspace(workspace, workspace_bytes, need);
+  if (rc != CECA_OK) return rc;
+  if (overlaps(E, tb, G, rb) || overlaps(tokens, (int64_t)n * T * 4, E, tb)) return fail(CECA_EINVAL, "E overlaps an input");
+  ceca::EmbedArgs a{};
+  a.dE = E;  a.lde = lde;  a.ldr = ldr;  a.tokens = tokens;  a.rows = const_cast<void*>(G);  a.ldo = ldg;
+  a.n = n;  a.V = V;  a.h = h;  a.T = T;  a.type = type;  a.scale = scale;  a.accumulate = accumulate != 0;
+  const hipError_t e = ceca::launch_embed_grad(a, (hipStream_t)hip_stream);
+  return e == hipSuccess ? CECA_OK : hip_fail(e, "embedding gradient kernel launch");
+}
+
+int64_t ceca_distill_workspace_bytes(const ceca_distill_t* spec) {
+  const int32_t rc = check_distill(spec);
+  if (rc != CECA_OK) return rc;
+  return 0;
+}
+
+int32_t ceca_distill(const ceca_distill_t* spec, float* loss, void* grad, int64_t ldg, void* workspace, int64_t workspace_bytes,
+                     void* hip_stream) {
+  const int64_t need = ceca_distill_workspace_bytes(spec);
+  if (need < 0) return (int32_t)need;
+  const ceca_distill_t& p = *spec;
+  if (p.T == 0) return CECA_OK;
+  if (!loss && !grad) return fail(CECA_EINVAL, "neither loss nor gradient asked for");
+  if (grad && ldg < p.V) return fail(CECA_EINVAL, "need V <= ldg (V = %d, ldg = %lld)", p.V, (long long)ldg);
+  const int64_t size = elem_size(p.type), rows = (int64_t)p.n * p.T;
+  if (!on_elements(loss, 4) || !on_elements(grad, size)) return fail(CECA_EINVAL, "pointers must lie on element boundaries");
+  int64_t sb, gb;
+  if (!span_bytes(rows, p.ld, p.V, size, &sb) || !span_bytes(rows, grad ? ldg : 0, p.V, size, &gb)) return fail(CECA_EINVAL, "sizes beyond the address space");
+  const struct { const void* p; int64_t bytes; } in[] = {
+      {p.logits, sb}, {p.top, rows * p.K * 4}, {p.ids, rows * p.K * 4}, {p.peer, 4 * (int64_t)p.n}, {p.labels, rows * 4}, {p.weight, rows * 4}};
+  for (const auto& b : in) {
+    if (!b.p) continue;
+    const bool itself = b.p == p.logits && grad == p.logits && ldg == p.ld;
+    if (grad && !itself && overlaps(grad, gb, b.p, b.bytes)) return fail(CECA_EINVAL, "the gradient overlaps an input");
+    if (loss && overlaps(loss, rows * 4, b.p, b.bytes)) return fail(CECA_EINVAL, "the loss overlaps an input");
+  }
+  if (loss && grad && overlaps(loss, rows * 4, grad, gb)) return fail(CECA_EINVAL, "the loss overlaps the gradient");
+  const int32_t rc = check_workspace(workspace, workspace_bytes, need);
+  if (rc != CECA_OK) return rc;
+  ceca::DistillArgs a{};
+  a.logits = p.logits;  a.ld = p.ld;  a.grad = grad;  a.ldg = ldg;  a.loss = loss;
+  a.top = p.top;  a.ids = p.ids;  a.peer = p.peer;  a.labels = p.hard > 0.0f ? p.labels : nullptr;  a.weight = p.weight;
+  a.n = p.n;  a.T = p.T;  a.V = p.V;  a.K = p.K;  a.type = p.type;  a.tau = p.temperature;  a.hard = p.hard;
+  const hipError_t e = ceca::launch_distill(a, (hipStream_t)hip_stream);
+  return e == hipSuccess ? CECA_OK : hip_fail(e, "distillation kernel launch");
+}
+
+int64_t ceca_top_logits_workspace_bytes(int32_t type, int32_t rows, int32_t V, int32_t K) {
+  const int32_t rc = check_top(type, rows, V, K);
+  if (rc != CECA_OK) return rc;
+  return 0;
+}
+
+int32_t ceca_top_logits(const void* logits, int32_t type, int64_t ld, int32_t rows, int32_t V, int32_t K, float* top, int32_t* ids,
+                        void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  const int64_t need = ceca_top_logits_workspace_bytes(type, rows, V, K);
+  if (need < 0) return (int32_t)need;
+  if (ld < V) return fail(CECA_EINVAL, "need V <= ld (V = %d, ld = %lld)", V, (long long)ld);
+  if (rows == 0) return CECA_OK;
+  if (!logits || !top || !ids) return fail(CECA_EINVAL, "null pointer");
+  const int64_t size = elem_size(type), out = (int64_t)rows * K * 4;
+  if (!on_elements(logits, size) || !on_elements(top, 4) || !on_elements(ids, 4)) return fail(CECA_EINVAL, "pointers must lie on element boundaries");
+  int64_t sb;
+  if (!span_bytes(rows, ld, V, size, &sb)) return fail(CECA_EINVAL, "sizes beyond the address space");
+  if (overlaps(logits, sb, top, out) || overlaps(logits, sb, ids, out) || overlaps(top, out, ids, out))
+    return fail(CECA_EINVAL, "an output overlaps the logits or the other output");
+  const int32_t rc = check_workspace(workspace, workspace_bytes, need);
+  if (rc != CECA_OK) return rc;
+  ceca::TopArgs a{};
+  a.logits = logits;  a.ld = ld;  a.top = top;  a.ids = ids;
+  a.rows = rows;  a.V = V;  a.K = K;  a.type = type;
+  const hipError_t e = ceca::launch_top(a, (hipStream_t)hip_stream);
+  return e == hipSuccess ? CECA_OK : hip_fail(e, "top logits kernel launch");
 }
 
 int32_t ceca_describe_step_launch(int32_t n, int64_t d, int64_t ld, int32_t r, int32_t port, int32_t kind,
