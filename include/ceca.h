@@ -328,7 +328,7 @@ enum { CECA_F32 = 0, CECA_BF16 = 1, CECA_F16 = 2 };
  * E: device, agent i's table is V rows of h floats, ldr apart, from E + i lde on -- a part of row i of a state, say.
  * tokens: device, n T int32; one outside [0, V) stands for padding: a row of zeros.
  * out: device, n T rows of h elements of `type`, ldo apart; disjoint from E and tokens.
- * Needs h <= ldr <= 2^31 - 1, h <= ldo, and lde >= (V - 1) ldr + h with more than one agent. */
+ * Needs h <= ldr <= 2^31 - 1, h <= 2^30, h <= ldo, and lde >= (V - 1) ldr + h with more than one agent. */
 int32_t ceca_embed(const float* E, int64_t lde, int64_t ldr, int32_t n, int32_t V, int32_t h, const int32_t* tokens, int32_t T,
                    float scale, void* out, int32_t type, int64_t ldo, void* hip_stream);
 
@@ -364,7 +364,8 @@ int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t*
  *     loss and the gradient at its entries' places. */
 #define CECA_TOP_MAX 256
 typedef struct {
-  int32_t n, T, V;
+  int32_t n, T;
+  int32_t V;               /* 1 .. 2^30 */
   int32_t K;               /* entries per position, 0 .. CECA_TOP_MAX */
   int32_t type;            /* of the logits and of the gradient */
   float temperature;       /* 0.001 .. 1000 */
@@ -392,7 +393,7 @@ int32_t ceca_distill(const ceca_distill_t* spec, float* loss, void* grad, int64_
 /* Bytes of device workspace ceca_top_logits needs (may be 0); < 0 on error. */
 int64_t ceca_top_logits_workspace_bytes(int32_t type, int32_t rows, int32_t V, int32_t K);
 
-/* The K largest (1 .. CECA_TOP_MAX) of every row's V logits, from the largest down, the lower place first among equals
+/* The K largest (1 .. CECA_TOP_MAX) of every row's V logits (V up to 2^30), from the largest down, the lower place first among equals
  * (-0 equals +0; NaN counts above +inf): top (device, rows K floats) and ids (device, rows K int32).  Logits of -inf are
  * masked: where fewer than K others are there, -inf and the place -1 fill up, which ceca_distill takes as no entry.
  * logits: device, `rows` rows of V elements of `type`, ld apart; top and ids are disjoint from it and from each other.

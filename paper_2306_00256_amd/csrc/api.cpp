@@ -615,6 +615,7 @@ bool on_elements(const void* p, int64_t size) { return (reinterpret_cast<uintptr
 // Bytes from the first to the last element of `rows` rows of `width` elements, `pitch` apart; 0 without rows.
 // (More than 2^47 bytes lie beyond any device's memory; the product must not overflow.)
 constexpr int64_t kMostBytes = 1LL << 47;
+constexpr int32_t kMostColumns = 1 << 30;      // kernels count columns in 32 bits, past the end of a row by a tile
 bool span_bytes(int64_t rows, int64_t pitch, int64_t width, int64_t size, int64_t* bytes) {
   *bytes = 0;
   if (rows == 0) return true;
@@ -627,6 +628,7 @@ bool span_bytes(int64_t rows, int64_t pitch, int64_t width, int64_t size, int64_
 int32_t check_tables(const void* E, int64_t lde, int64_t ldr, int32_t n, int32_t V, int32_t h, const void* rows, int32_t type, int64_t ldo,
                      const void* tokens, int32_t T, int64_t* table_bytes, int64_t* row_bytes) {
   if (n < 1 || V < 1 || h < 1 || T < 0) return fail(CECA_EINVAL, "need n, V, h >= 1 and T >= 0 (n = %d, V = %d, h = %d, T = %d)", n, V, h, T);
+  if (h > kMostColumns) return fail(CECA_EINVAL, "h = %d: rows of at most 2^30 columns", h);
   if ((int64_t)n * T > INT32_MAX) return fail(CECA_EINVAL, "n T = %lld: need fewer than 2^31 positions", (long long)n * T);
   if (type < CECA_F32 || type > CECA_F16) return fail(CECA_EINVAL, "unknown element type %d", type);
   if (!E || (T > 0 && (!rows || !tokens))) return fail(CECA_EINVAL, "null pointer");
@@ -650,6 +652,7 @@ int32_t check_workspace(const void* workspace, int64_t have, int64_t need) {
 
 int32_t check_distill(const ceca_distill_t* p) {
   if (!p) return fail(CECA_EINVAL, "null pointer");
+  if (p->V > kMostColumns) return fail(CECA_EINVAL, "V = %d: rows of at most 2^30 logits", p->V);
   if (p->n < 1 || p->V < 1 || p->T < 0) return fail(CECA_EINVAL, "need n, V >= 1 and T >= 0 (n = %d, V = %d, T = %d)", p->n, p->V, p->T);
   if ((int64_t)p->n * p->T > INT32_MAX) return fail(CECA_EINVAL, "n T = %lld: need fewer than 2^31 positions", (long long)p->n * p->T);
   if (p->type < CECA_F32 || p->type > CECA_F16) return fail(CECA_EINVAL, "unknown element type %d", p->type);
@@ -666,6 +669,7 @@ int32_t check_distill(const ceca_distill_t* p) {
 }
 
 int32_t check_top(int32_t type, int32_t rows, int32_t V, int32_t K) {
+  if (V > kMostColumns) return fail(CECA_EINVAL, "V = %d: rows of at most 2^30 logits", V);
   if (rows < 0 || V < 1) return fail(CECA_EINVAL, "need rows >= 0 and V >= 1 (rows = %d, V = %d)", rows, V);
   if (type < CECA_F32 || type > CECA_F16) return fail(CECA_EINVAL, "unknown element type %d", type);
   if (K < 1 || K > CECA_TOP_MAX) return fail(CECA_EINVAL, "K = %d outside [1, %d]", K, CECA_TOP_MAX);
@@ -1408,9 +1412,10 @@ int32_t ceca_embed(const float* E, int64_t lde, int64_t ldr, int32_t n, int32_t 
 }
 
 int64_t ceca_embed_grad_workspace_bytes(int32_t n, int32_t V, int32_t h, int32_t T) {
-  if (n < 1 || V < 1 || h < 1 || T < 0 || (int64_t)n * T > INT32_MAX)
-    return fail(CECA_EINVAL, "need n, V, h >= 1, T >= 0 and n T < 2^31 (n = %d, V = %d, h = %d, T = %d)", n, V, h, T);
-  return 0;
+  if (n < 1 || V < 1 || h < 1 || h > kMostColumns || T < 0 || (int64_t)n * T > INT32_MAX)
+    return fail(CECA_EINVAL, "need n, V >= 1, 1 <= h <= 2^30, T >= 0 and n T < 2^31 (n = %d, V = %d, h = %d, T = %d)", n, V, h, T);
+  if ((__int128)n * T * h > kMostBytes) return fail(CECA_EINVAL, "sizes beyond the address space");
+  return ceca::plan_embed_grad(n, V, h, T).bytes;
 }
 
 int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t* tokens, int32_t T, float scale, int32_t accumulate,
@@ -1420,12 +1425,15 @@ int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t*
   int32_t rc = check_tables(E, lde, ldr, n, V, h, G, type, ldg, tokens, T, &tb, &rb);
   if (rc != CECA_OK) return rc;
   const int64_t need = ceca_embed_grad_workspace_bytes(n, V, h, T);
+  if (need < 0) return (int32_t)need;
   rc = check_workspace(workspace, workspace_bytes, need);
   if (rc != CECA_OK) return rc;
   if (overlaps(E, tb, G, rb) || overlaps(tokens, (int64_t)n * T * 4, E, tb)) return fail(CECA_EINVAL, "E overlaps an input");
+  if (overlaps(workspace, need, G, rb) || overlaps(workspace, need, tokens, (int64_t)n * T * 4) || overlaps(workspace, need, E, tb))
+    return fail(CECA_EINVAL, "the workspace overlaps an argument");
   ceca::EmbedArgs a{};
   a.dE = E;  a.lde = lde;  a.ldr = ldr;  a.tokens = tokens;  a.rows = const_cast<void*>(G);  a.ldo = ldg;
-  a.n = n;  a.V = V;  a.h = h;  a.T = T;  a.type = type;  a.scale = scale;  a.accumulate = accumulate != 0;
+  a.n = n;  a.V = V;  a.h = h;  a.T = T;  a.type = type;  a.scale = scale;  a.accumulate = accumulate != 0;  a.workspace = workspace;
   const hipError_t e = ceca::launch_embed_grad(a, (hipStream_t)hip_stream);
   return e == hipSuccess ? CECA_OK : hip_fail(e, "embedding gradient kernel launch");
 }

@@ -1,4 +1,6 @@
-// Embedding lookup in the agents' tables, and its gradient.
+// Embedding lookup in the agents' tables, and its gradient by sorted tokens.
+#include <algorithm>
+
 #include "device_util.h"
 #include "text_util.h"
 
@@ -9,66 +11,537 @@ namespace {
 // out[i, t, :] = scale * E_i[token, :], one wavefront per position; zeros where the token is none of the vocabulary.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-  if (row >= (int64_t)a.n * a.T) return;
-  const int32_t token = a.tokens[row];
-  const bool real = token >= 0 && token < a.V;
-  const float* e = a.E + row / a.T * a.lde + (real ? token : 0) * a.ldr;
-  T* out = static_cast<T*>(a.rows) + row * a.ldo;
-  for (int32_t c = threadIdx.x % 64; c < a.h; c += 64) out[c] = from_float<T>(real ? a.scale * e[c] : 0.0f);
+  const int64_t rows = (int64_t)a.n * a.T;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < rows; row += (int64_t)gridDim.x * 4) {
+    const int32_t token = a.tokens[row];
+    const bool real = token >= 0 && token < a.V;
+    const float* e = a.E + row / a.T * a.lde + (real ? token : 0) * a.ldr;
+    T* out = static_cast<T*>(a.rows) + row * a.ldo;
+    for (int32_t c = threadIdx.x % 64; c < a.h; c += 64) out[c] = from_float<T>(real ? a.scale * e[c] : 0.0f);
+  }
 }
 
-// e_i[v, :] = scale * sum of the gradient's rows at v's positions, in their order: one wavefront per row of a table
-// goes through the agent's tokens.
-template <typename T>
-__global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs a) {
-  const int64_t vrow = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-  if (vrow >= (int64_t)a.n * a.V) return;
-  const int lane = threadIdx.x % 64;
-  const int64_t i = vrow / a.V;
-  const int32_t v = (int32_t)(vrow - i * a.V);
-  const int32_t* tokens = a.tokens + i * a.T;
-  const T* g = static_cast<const T*>(a.rows) + i * a.T * a.ldo;
-  float* e = a.dE + i * a.lde + v * a.ldr;
-  for (int32_t c0 = 0; c0 < a.h; c0 += 64) {
-    const int32_t c = c0 + lane;
-    float sum = 0.0f;
-    bool some = false;
-    for (int32_t t0 = 0; t0 < a.T; t0 += 64) {
-      uint64_t hits = __ballot(t0 + lane < a.T && tokens[min(t0 + lane, a.T - 1)] == v);
-      some |= hits != 0;
-      for (; hits; hits &= hits - 1) {
-        const int64_t t = t0 + __builtin_ctzll(hits);
-        if (c < a.h) sum += to_float(g[t * a.ldo + c]);
+// ---- the gradient ----
+// e_i[v, :] = scale * sum of G's rows at v's positions.  A position's row is read once, a table's row is written once: what bounds
+// it is the memory's rate, mostly for the zeros of rows whose tokens do not occur.  Three launches:
+//   sort   positions into the order of (token, position), in LDS; the other workgroups of the same launch write the zeros, so
+//          that neither waits for the other
+//   walk   a wavefront adds the rows of kChunk sorted positions up, in order; where a token's positions lie in one chunk its row
+//          of the table is done, else the chunk's share goes to the workspace
+//   join   the shares of tokens that lie in several chunks, in their order
+// Which lane adds what follows from the tokens alone: no atomics, the same bits every time.
+
+// Zeros over `count` floats, by THREADS threads.
+constexpr int64_t kFillFloats = 32768;
+
+template <int THREADS>
+__device__ __forceinline__ void fill_zeros(float* p, int64_t count) {
+  const vf4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+  const int64_t groups = count / 4;
+  for (int64_t g = threadIdx.x; g < groups; g += THREADS) st_stream<vf4>(p + 4 * g, zero);
+  const int64_t c = groups * 4 + threadIdx.x;
+  if (c < count) p[c] = 0.0f;
+}
+
+// Part `part` of the tables: runs of rows, as one piece where nothing lies between them.
+template <int THREADS>
+__device__ __forceinline__ void fill_part(const EmbedArgs& a, int64_t part, int32_t run, int64_t runs) {
+  const int64_t i = part / runs;
+  const int32_t v0 = (int32_t)(part - i * runs) * run, v1 = (int32_t)min((int64_t)v0 + run, (int64_t)a.V);
+  float* e = a.dE + i * a.lde;
+  if (a.ldr == a.h) {
+    fill_zeros<THREADS>(e + v0 * a.ldr, (int64_t)(v1 - v0) * a.h);
+  } else {
+    for (int32_t v = v0; v < v1; ++v) fill_zeros<THREADS>(e + v * a.ldr, a.h);
+  }
+}
+
+// One stable pass over up to IPT * 1024 keys by `bits` bits from `shift` on: where every key of this thread goes.  A wavefront
+// owns a block of 64 IPT keys, key j * 64 + lane of it is the lane's j-th; lanes with the same digit find each other by ballots,
+// and a digit's count per wavefront is kept in `count` (16 x digits).
+template <int IPT>
+__device__ __forceinline__ void rank_keys(const uint32_t (&key)[IPT], uint32_t (&to)[IPT], int shift, int bits, uint32_t* count, uint32_t* totals) {
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, digits = 1 << bits;
+  for (int k = tid; k < 16 * digits; k += 1024) count[k] = 0;
+  __syncthreads();
+  uint32_t* mine = count + wave * digits;
+#pragma unroll
+  for (int j = 0; j < IPT; ++j) {
+    const uint32_t d = key[j] >> shift & (digits - 1);
+    uint64_t same = ~0ull;
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t has = __ballot(d >> b & 1);
+      same &= d >> b & 1 ? has : ~has;
+    }
+    const uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+    const uint32_t seen = mine[d];
+    __builtin_amdgcn_wave_barrier();
+    if (before == 0) mine[d] = seen + (uint32_t)__builtin_popcountll(same);
+    __builtin_amdgcn_wave_barrier();
+    to[j] = seen + before;
+  }
+  __syncthreads();
+  // exclusive sums in the order (digit, wavefront): 16 digits' counts a thread chunk, then over the threads
+  const int per = 16 * digits / 1024 > 0 ? 16 * digits / 1024 : 1;
+  const int first = tid * per;                         // entry e stands for digit e / 16 of wavefront e % 16
+  uint32_t sum = 0;
+  if (first < 16 * digits)
+    for (int e = first; e < first + per; ++e) sum += count[(e % 16) * digits + e / 16];
+  uint32_t upto = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t x = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 63) totals[wave] = upto;
+  __syncthreads();
+  uint32_t base = upto - sum;
+  for (int w = 0; w < wave; ++w) base += totals[w];
+  if (first < 16 * digits)
+    for (int e = first; e < first + per; ++e) {
+      const int at = (e % 16) * digits + e / 16;
+      const uint32_t x = count[at];
+      count[at] = base;
+      base += x;
+    }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < IPT; ++j) to[j] += mine[key[j] >> shift & (digits - 1)];
+}
+
+struct SortArgs {
+  EmbedArgs e;
+  EmbedGradPlan p;
+  int32_t run;                // rows per part of the fill
+  int64_t runs, sorts, parts; // parts per table, workgroups that sort, parts in all (0: nothing is filled)
+};
+
+// Agents' positions sorted by one workgroup each: the keys are (token, position) in one word, so that LDS holds up to 16384 of
+// them beside the counts.
+template <int IPT>
+__global__ __launch_bounds__(1024) void sort_lds_kernel(SortArgs s) {
+  extern __shared__ uint32_t lds[];
+  const EmbedArgs& a = s.e;
+  if ((int64_t)blockIdx.x >= s.sorts) {
+    for (int64_t part = blockIdx.x - s.sorts; part < s.parts; part += gridDim.x - s.sorts) fill_part<1024>(a, part, s.run, s.runs);
+    return;
+  }
+  uint32_t* count = lds;                               // 16 x digits
+  uint32_t* totals = lds + 16 * kDigits;
+  uint32_t* keys = totals + 16;                        // IPT * 1024
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  for (int64_t i = blockIdx.x; i < a.n; i += s.sorts) {
+    const int32_t* tokens = a.tokens + i * a.T;
+    uint32_t key[IPT], to[IPT];
+    const uint32_t none = (uint32_t)((((uint64_t)1 << (s.p.bits + s.p.pos_bits)) - 1));
+#pragma unroll
+    for (int j = 0; j < IPT; ++j) {
+      const int t = (wave * IPT + j) * 64 + lane;
+      const int32_t v = t < a.T ? tokens[t] : -1;
+      // places past the last position go last of all: the largest key, and behind the others of it
+      key[j] = t < a.T ? (uint32_t)(v >= 0 && v < a.V ? v : a.V) << s.p.pos_bits | (uint32_t)t : none;
+    }
+    for (int shift = 0; shift < s.p.bits; shift += kDigitBits) {
+      const int bits = min(kDigitBits, s.p.bits - shift);
+      rank_keys<IPT>(key, to, s.p.pos_bits + shift, bits, count, totals);
+#pragma unroll
+      for (int j = 0; j < IPT; ++j) keys[to[j]] = key[j];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < IPT; ++j) key[j] = keys[(wave * IPT + j) * 64 + lane];
+    }
+    uint32_t* tok = reinterpret_cast<uint32_t*>(static_cast<char*>(a.workspace) + s.p.tok0) + i * a.T;
+    uint32_t* pos = reinterpret_cast<uint32_t*>(static_cast<char*>(a.workspace) + s.p.pos0) + i * a.T;
+#pragma unroll
+    for (int j = 0; j < IPT; ++j) {
+      const int t = (wave * IPT + j) * 64 + lane;
+      if (t < a.T) {
+        tok[t] = min(key[j] >> s.p.pos_bits, (uint32_t)a.V);
+        pos[t] = key[j] & (((uint32_t)1 << s.p.pos_bits) - 1);
       }
     }
-    if (c < a.h) {
-      if (!a.accumulate) e[c] = a.scale * sum;
-      else if (some) e[c] += a.scale * sum;
+    __syncthreads();
+  }
+}
+
+// Longer sequences: tiles of kTile positions, one pass of kDigitBits bits in two launches.  Counts of every tile first ...
+struct PassArgs {
+  const int32_t* tokens;       // first pass, else null
+  const uint32_t *tok, *pos;   // later passes
+  uint32_t *tok_out, *pos_out, *hist;
+  int32_t n, V, T, tiles, shift, bits;
+};
+__device__ __forceinline__ uint32_t pass_key(const PassArgs& p, int64_t i, int64_t t) {
+  if (!p.tokens) return p.tok[i * p.T + t];
+  const int32_t v = p.tokens[i * p.T + t];
+  return (uint32_t)(v >= 0 && v < p.V ? v : p.V);
+}
+__global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p, EmbedArgs a, int32_t run, int64_t runs, int64_t part0, int64_t part1) {
+  __shared__ uint32_t count[kDigits];
+  const int64_t sorts = (int64_t)p.n * p.tiles;
+  for (int64_t b = blockIdx.x; b < sorts + part1 - part0; b += gridDim.x) {
+    if (b >= sorts) {
+      fill_part<1024>(a, part0 + b - sorts, run, runs);
+      continue;
+    }
+    const int64_t i = b / p.tiles, t0 = (b - i * p.tiles) * kTile;
+    if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
+    __syncthreads();
+    for (int64_t t = t0 + threadIdx.x; t < min(t0 + kTile, (int64_t)p.T); t += 1024)
+      atomicAdd(&count[pass_key(p, i, t) >> p.shift & ((1u << p.bits) - 1)], 1u);       // whole numbers: any order
+    __syncthreads();
+    if (threadIdx.x < kDigits) p.hist[b * kDigits + threadIdx.x] = count[threadIdx.x];
+    __syncthreads();
+  }
+}
+// ... then every tile's keys to their places: behind the smaller digits of all tiles and the same digit's of earlier tiles.
+__global__ __launch_bounds__(1024) void place_keys_kernel(PassArgs p, EmbedArgs a, int32_t run, int64_t runs, int64_t part0, int64_t part1) {
+  constexpr int IPT = kTile / 1024;
+  __shared__ uint32_t count[16 * kDigits], totals[16], base[kDigits], sums[16];
+  const int64_t sorts = (int64_t)p.n * p.tiles;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  for (int64_t b = blockIdx.x; b < sorts + part1 - part0; b += gridDim.x) {
+    if (b >= sorts) {
+      fill_part<1024>(a, part0 + b - sorts, run, runs);
+      continue;
+    }
+    const int64_t i = b / p.tiles;
+    const int32_t tile = (int32_t)(b - i * p.tiles);
+    uint32_t before = 0, all = 0;
+    if (tid < kDigits)
+      for (int32_t k = 0; k < p.tiles; ++k) {
+        const uint32_t c = p.hist[(i * p.tiles + k) * kDigits + tid];
+        all += c;
+        before += k < tile ? c : 0;
+      }
+    uint32_t upto = all;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t x = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    uint32_t start = upto - all + before;
+    for (int w = 0; w < wave; ++w) start += sums[w];
+    if (tid < kDigits) base[tid] = start;
+    uint32_t key[IPT], pos[IPT], to[IPT];
+    const uint32_t none = 0xffffffffu;
+#pragma unroll
+    for (int j = 0; j < IPT; ++j) {
+      const int64_t t = (int64_t)tile * kTile + (wave * IPT + j) * 64 + lane;
+      key[j] = t < p.T ? pass_key(p, i, t) : none;
+      pos[j] = t < p.T ? (p.tokens ? (uint32_t)t : p.pos[i * p.T + t]) : none;
+    }
+    rank_keys<IPT>(key, to, p.shift, p.bits, count, totals);
+    // to: the place among the tile's keys; `count` of wavefront 0 is now where a digit begins among them
+#pragma unroll
+    for (int j = 0; j < IPT; ++j) {
+      const uint32_t d = key[j] >> p.shift & ((1u << p.bits) - 1);
+      if (pos[j] != none) {
+        const int64_t at = i * p.T + base[d] + (to[j] - count[d]);
+        p.tok_out[at] = key[j];
+        p.pos_out[at] = pos[j];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// A lane's columns of one row: VEC of them from column c on, the last VEC where fewer are left (it stores its own alone).
+template <typename T, int VEC> struct Columns {
+  int32_t c, at, h;           // first own column, first column read
+  bool whole, some;
+  __device__ __forceinline__ Columns(int32_t first, int32_t h_) : c(first), at(min(first, h_ - VEC)), h(h_), whole(first + VEC <= h_), some(first < h_) {}
+  __device__ __forceinline__ void store(float* row, const float (&x)[VEC]) const {
+    if (whole) {
+      Pack<float, VEC> v;
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) v.v[k] = x[k];
+      v.store(row + at);
+    } else if (some) {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) if (at + k >= c) row[at + k] = x[k];
+    }
+  }
+};
+
+struct WalkArgs {
+  EmbedArgs e;
+  const uint32_t *tok, *pos;
+  float* partial;
+  int64_t pitch;
+  int32_t chunks, tiles;      // chunks per agent, column tiles
+};
+
+constexpr int kAhead = 8;     // rows whose loads are in flight
+
+// One wavefront per chunk of sorted positions and tile of 64 VEC columns.
+template <typename T, int VEC, bool ADD>
+__global__ __launch_bounds__(256) void walk_kernel(WalkArgs w) {
+  const EmbedArgs& a = w.e;
+  const int lane = threadIdx.x % 64;
+  const int64_t units = (int64_t)a.n * w.chunks * w.tiles;
+  for (int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); unit < units; unit += (int64_t)gridDim.x * 4) {
+    const int64_t ic = unit / w.tiles, i = ic / w.chunks;
+    const int32_t chunk = (int32_t)(ic - i * w.chunks);
+    const Columns<T, VEC> col((int32_t)(unit - ic * w.tiles) * 64 * VEC + lane * VEC, a.h);
+    const T* G = static_cast<const T*>(a.rows) + i * a.T * a.ldo + col.at;
+    float* E = a.dE + i * a.lde;
+    float* part = w.partial + ic * 2 * w.pitch;
+    // lane l holds sorted place first - 1 + l: the one before the chunk, the chunk, the one behind it
+    const int32_t first = chunk * kChunk, place = first - 1 + lane;
+    const bool there = place >= 0 && place < a.T && lane <= kChunk + 1;
+    const uint32_t tok = there ? w.tok[i * a.T + place] : 0xffffffffu;
+    const uint32_t pos = there && tok < (uint32_t)a.V ? w.pos[i * a.T + place] : 0;
+    uint32_t last = __builtin_amdgcn_readlane(tok, 0);          // the token before
+    bool begun = false;                                          // whether the token at hand began in an earlier chunk
+    float sum[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) sum[k] = 0.0f;
+    for (int j0 = 0; j0 < kChunk; j0 += kAhead) {
+      if (__builtin_amdgcn_readlane(tok, 1 + j0) >= (uint32_t)a.V) break;        // padding sorts last
+      Pack<T, VEC> g[kAhead];
+      Pack<float, VEC> old[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const uint32_t v = __builtin_amdgcn_readlane(tok, 1 + j0 + j);
+        if (v < (uint32_t)a.V) {
+          if (col.some) g[j] = Pack<T, VEC>::load_stream(G + (int64_t)__builtin_amdgcn_readlane(pos, 1 + j0 + j) * a.ldo);
+          if (ADD && v != __builtin_amdgcn_readlane(tok, 2 + j0 + j)) {
+            if (col.some) old[j] = Pack<float, VEC>::load(E + (int64_t)v * a.ldr + col.at);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const uint32_t v = __builtin_amdgcn_readlane(tok, 1 + j0 + j), next = __builtin_amdgcn_readlane(tok, 2 + j0 + j);
+        if (v < (uint32_t)a.V) {
+          if (v != last || j0 + j == 0) {
+            begun = v == last;
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) sum[k] = 0.0f;
+          }
+          last = v;
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) sum[k] += g[j].get(k);
+          const bool ends = next != v;
+          if (ends && !begun) {
+            float x[VEC];
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) x[k] = ADD ? __builtin_fmaf(a.scale, sum[k], old[j].get(k)) : a.scale * sum[k];
+            col.store(E + (int64_t)v * a.ldr, x);
+          } else if (ends || j0 + j == kChunk - 1) {
+            col.store(part + (begun ? 0 : w.pitch), sum);       // (where one token fills the chunk from and to elsewhere: once)
+          }
+        }
+      }
     }
   }
 }
+
+// One wavefront per chunk and tile of columns: the token that begins in the chunk and goes on behind it.
+template <int VEC, bool ADD>
+__global__ __launch_bounds__(256) void join_kernel(WalkArgs w) {
+  const EmbedArgs& a = w.e;
+  const int lane = threadIdx.x % 64;
+  const int64_t units = (int64_t)a.n * (w.chunks - 1) * w.tiles;
+  for (int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); unit < units; unit += (int64_t)gridDim.x * 4) {
+    const int64_t ic = unit / w.tiles, i = ic / (w.chunks - 1);
+    const int32_t chunk = (int32_t)(ic - i * (w.chunks - 1));
+    const uint32_t* tok = w.tok + i * a.T;
+    const int32_t end = (chunk + 1) * kChunk;            // a place there is: this is not the last chunk
+    const uint32_t v = tok[end - 1];
+    if (v >= (uint32_t)a.V || tok[end] != v) continue;
+    if (chunk > 0 && tok[chunk * kChunk - 1] == v) continue;    // it began earlier
+    const Columns<float, VEC> col((int32_t)(unit - ic * w.tiles) * 64 * VEC + lane * VEC, a.h);
+    const float* part = w.partial + (i * w.chunks + chunk) * 2 * w.pitch;
+    float sum[VEC];
+    {
+      const Pack<float, VEC> p = Pack<float, VEC>::load(part + w.pitch + (col.some ? col.at : 0));
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) sum[k] = p.get(k);
+    }
+    for (int32_t c = chunk + 1; c < w.chunks; c += 64) {
+      // chunks that begin with the token: a run of them, its end by ballot
+      const uint64_t mine = __ballot(c + lane < w.chunks && tok[(int64_t)min(c + lane, w.chunks - 1) * kChunk] == v);
+      const int32_t run = mine == ~0ull ? 64 : __builtin_ctzll(~mine);
+      for (int32_t k0 = 0; k0 < run; k0 += kAhead) {
+        Pack<float, VEC> p[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+          p[j] = Pack<float, VEC>::load(part + (int64_t)(c - chunk + min(k0 + j, run - 1)) * 2 * w.pitch + (col.some ? col.at : 0));
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+          if (k0 + j < run) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) sum[k] += p[j].get(k);
+          }
+      }
+      if (run < 64) break;
+    }
+    float* row = a.dE + i * a.lde + (int64_t)v * a.ldr;
+    if (col.some) {
+      const Pack<float, VEC> old = ADD ? Pack<float, VEC>::load(row + col.at) : Pack<float, VEC>{};
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) sum[k] = ADD ? __builtin_fmaf(a.scale, sum[k], old.get(k)) : a.scale * sum[k];
+      col.store(row, sum);
+    }
+  }
+}
+
+// Up to 64 NT positions: a wavefront holds all of an agent's tokens, NT a lane.  The first position of each token adds up its
+// rows; other wavefronts write the zeros of rows that none of the tokens names.  One launch.
+template <typename T, int VEC, int NT, bool ADD>
+__global__ __launch_bounds__(256) void few_positions_kernel(EmbedArgs a, int32_t tiles, int32_t run, int64_t runs) {
+  const int lane = threadIdx.x % 64;
+  const int64_t sums = (int64_t)a.n * a.T * tiles, units = sums + (ADD ? 0 : a.n * runs);
+  for (int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); unit < units; unit += (int64_t)gridDim.x * 4) {
+    const bool adds = unit < sums;
+    const int64_t i = adds ? unit / ((int64_t)a.T * tiles) : (unit - sums) / runs;
+    int32_t tok[NT];
+#pragma unroll
+    for (int k = 0; k < NT; ++k) tok[k] = k * 64 + lane < a.T ? a.tokens[i * a.T + k * 64 + lane] : -1;
+    if (adds) {
+      const int32_t rest = (int32_t)(unit - i * ((int64_t)a.T * tiles)), t = rest / tiles;
+      const int32_t v = a.tokens[i * a.T + t];
+      if (v < 0 || v >= a.V) continue;
+      uint64_t hits[NT];
+      bool earlier = false;
+#pragma unroll
+      for (int k = 0; k < NT; ++k) {
+        hits[k] = __ballot(tok[k] == v);
+        earlier |= t > k * 64 && (hits[k] & (t - k * 64 >= 64 ? ~0ull : (1ull << (t - k * 64)) - 1)) != 0;
+      }
+      if (earlier) continue;
+      const Columns<T, VEC> col((rest - t * tiles) * 64 * VEC + lane * VEC, a.h);
+      if (!col.some) continue;
+      const T* G = static_cast<const T*>(a.rows) + i * a.T * a.ldo + col.at;
+      float* row = a.dE + i * a.lde + (int64_t)v * a.ldr;
+      const Pack<float, VEC> old = ADD ? Pack<float, VEC>::load(row + col.at) : Pack<float, VEC>{};
+      float sum[VEC];
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) sum[c] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < NT; ++k)
+        for (uint64_t m = hits[k]; m; m &= m - 1) {
+          const Pack<T, VEC> g = Pack<T, VEC>::load(G + (int64_t)(k * 64 + __builtin_ctzll(m)) * a.ldo);
+#pragma unroll
+          for (int c = 0; c < VEC; ++c) sum[c] += g.get(c);
+        }
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) sum[c] = ADD ? __builtin_fmaf(a.scale, sum[c], old.get(c)) : a.scale * sum[c];
+      col.store(row, sum);
+    } else {
+      const int32_t v0 = (int32_t)(unit - sums - i * runs) * run, v1 = (int32_t)min((int64_t)v0 + run, (int64_t)a.V);
+      float* e = a.dE + i * a.lde;
+      bool some = false;
+#pragma unroll
+      for (int k = 0; k < NT; ++k) some |= __ballot(tok[k] >= v0 && tok[k] < v1) != 0;
+      const bool pieces = some || a.ldr != a.h;
+      for (int32_t v = v0; v < v1; v = pieces ? v + 1 : v1) {
+        bool named = false;
+        if (some) {
+#pragma unroll
+          for (int k = 0; k < NT; ++k) named |= __ballot(tok[k] == v) != 0;
+        }
+        if (named) continue;
+        float* p = e + v * a.ldr;
+        const int64_t count = pieces ? a.h : (int64_t)(v1 - v0) * a.h, groups = count / 4;
+        for (int64_t g = lane; g < groups; g += 64) st_stream<vf4>(p + 4 * g, vf4{0.0f, 0.0f, 0.0f, 0.0f});
+        if (groups * 4 + lane < count) p[groups * 4 + lane] = 0.0f;
+      }
+    }
+  }
+}
+
+constexpr int64_t kMostBlocks = 1 << 20;
+
+template <typename T> struct Lookup {
+  static hipError_t go(const EmbedArgs& a, hipStream_t st) {
+    const int64_t blocks = ((int64_t)a.n * a.T + 3) / 4;
+    embed_kernel<T><<<dim3((uint32_t)std::min(blocks, kMostBlocks)), dim3(256), 0, st>>>(a);
+    return hipGetLastError();
+  }
+};
+
+// Rows per part of the fill: about kFillFloats floats.
+int32_t run_of(const EmbedArgs& a, int64_t floats) { return (int32_t)std::max<int64_t>(std::min<int64_t>(floats / a.h, a.V), 1); }
+uint32_t four_a_block(int64_t units) { return (uint32_t)std::min((units + 3) / 4, kMostBlocks); }
+
+template <typename T, int VEC, int NT> hipError_t few_positions(const EmbedArgs& a, hipStream_t st) {
+  const int32_t tiles = (a.h + 64 * VEC - 1) / (64 * VEC), run = run_of(a, 4096);
+  const int64_t runs = (a.V + (int64_t)run - 1) / run;
+  const int64_t units = (int64_t)a.n * a.T * tiles + (a.accumulate ? 0 : a.n * runs);
+  if (units == 0) return hipSuccess;
+  if (a.accumulate) few_positions_kernel<T, VEC, NT, true><<<dim3(four_a_block(units)), dim3(256), 0, st>>>(a, tiles, run, runs);
+  else few_positions_kernel<T, VEC, NT, false><<<dim3(four_a_block(units)), dim3(256), 0, st>>>(a, tiles, run, runs);
+  return hipGetLastError();
+}
+
+template <int IPT> hipError_t sort_lds(const SortArgs& s, hipStream_t st) {
+  const size_t lds = (16 * kDigits + 16 + IPT * 1024) * sizeof(uint32_t);
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sort_lds_kernel<IPT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t fill = std::min<int64_t>(s.parts, 1 << 16);
+  sort_lds_kernel<IPT><<<dim3((uint32_t)(s.sorts + fill)), dim3(1024), lds, st>>>(s);
+  return hipGetLastError();
+}
+
+template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const EmbedGradPlan& p, hipStream_t st) {
+  if (p.small) return a.T <= 64 ? few_positions<T, VEC, 1>(a, st) : few_positions<T, VEC, 4>(a, st);
+  char* ws = static_cast<char*>(a.workspace);
+  auto words = [&](int64_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
+  SortArgs s{a, p, run_of(a, kFillFloats), 0, std::min<int64_t>(a.n, 1 << 16), 0};
+  s.runs = (a.V + (int64_t)s.run - 1) / s.run;
+  s.parts = a.accumulate ? 0 : a.n * s.runs;
+  uint32_t *tok = words(p.tok0), *pos = words(p.pos0);
+  hipError_t e = hipSuccess;
+  if (p.lds) {
+    e = a.T <= 1024 ? sort_lds<1>(s, st) : a.T <= 2048 ? sort_lds<2>(s, st) : a.T <= 4096 ? sort_lds<4>(s, st) : a.T <= 8192 ? sort_lds<8>(s, st) : sort_lds<16>(s, st);
+  } else {
+    const int passes = (p.bits + kDigitBits - 1) / kDigitBits;
+    uint32_t *tok2 = words(p.tok1), *pos2 = words(p.pos1);
+    for (int k = 0; k < passes && e == hipSuccess; ++k) {
+      PassArgs q{k ? nullptr : a.tokens, tok, pos, tok2, pos2, words(p.hist), a.n, a.V, a.T, p.tiles, k * kDigitBits, std::min(kDigitBits, p.bits - k * kDigitBits)};
+      // the zeros ride in the passes' launches, in equal shares
+      const int64_t cut[3] = {s.parts * (2 * k) / (2 * passes), s.parts * (2 * k + 1) / (2 * passes), s.parts * (2 * k + 2) / (2 * passes)};
+      const int64_t sorts = (int64_t)a.n * p.tiles;
+      count_digits_kernel<<<dim3((uint32_t)std::min(sorts + cut[1] - cut[0], kMostBlocks)), dim3(1024), 0, st>>>(q, a, s.run, s.runs, cut[0], cut[1]);
+      place_keys_kernel<<<dim3((uint32_t)std::min(sorts + cut[2] - cut[1], kMostBlocks)), dim3(1024), 0, st>>>(q, a, s.run, s.runs, cut[1], cut[2]);
+      e = hipGetLastError();
+      std::swap(tok, tok2);
+      std::swap(pos, pos2);
+    }
+  }
+  if (e != hipSuccess) return e;
+  WalkArgs w{a, tok, pos, reinterpret_cast<float*>(ws + p.partial), p.pitch, p.chunks, (a.h + 64 * VEC - 1) / (64 * VEC)};
+  const dim3 walk(four_a_block((int64_t)a.n * p.chunks * w.tiles)), join(four_a_block((int64_t)a.n * (p.chunks - 1) * w.tiles));
+  if (a.accumulate) {
+    walk_kernel<T, VEC, true><<<walk, dim3(256), 0, st>>>(w);
+    join_kernel<VEC, true><<<join, dim3(256), 0, st>>>(w);
+  } else {
+    walk_kernel<T, VEC, false><<<walk, dim3(256), 0, st>>>(w);
+    join_kernel<VEC, false><<<join, dim3(256), 0, st>>>(w);
+  }
+  return hipGetLastError();
+}
+
+template <typename T> struct Gradient {
+  static hipError_t go(const EmbedArgs& a, hipStream_t st) {
+    const EmbedGradPlan p = plan_embed_grad(a.n, a.V, a.h, a.T);
+    // short rows: enough lanes with columns of their own
+    return a.h > 128 ? gradient<T, 4>(a, p, st) : a.h > 64 ? gradient<T, 2>(a, p, st) : gradient<T, 1>(a, p, st);
+  }
+};
 
 template <template <typename> class Launch, typename... A> hipError_t by_type(int type, A... args) {
   if (type == TYPE_F32) return Launch<float>::go(args...);
   if (type == TYPE_BF16) return Launch<bf16_t>::go(args...);
   return Launch<_Float16>::go(args...);
 }
-
-template <typename T> struct Lookup {
-  static hipError_t go(const EmbedArgs& a, hipStream_t st) {
-    const int64_t blocks = ((int64_t)a.n * a.T + 3) / 4;
-    embed_kernel<T><<<dim3((uint32_t)blocks), dim3(256), 0, st>>>(a);
-    return hipGetLastError();
-  }
-};
-template <typename T> struct Gradient {
-  static hipError_t go(const EmbedArgs& a, hipStream_t st) {
-    const int64_t blocks = ((int64_t)a.n * a.V + 3) / 4;
-    embed_grad_kernel<T><<<dim3((uint32_t)blocks), dim3(256), 0, st>>>(a);
-    return hipGetLastError();
-  }
-};
 
 }  // namespace
 

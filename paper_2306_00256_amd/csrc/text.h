@@ -21,7 +21,43 @@ struct EmbedArgs {
   int32_t type;            // of rows
   float scale;
   int32_t accumulate;
+  void* workspace;         // of embed_grad_workspace bytes
 };
+
+// How the gradient's positions are brought into the order of their tokens, and its workspace.
+constexpr int kChunk = 32;             // sorted positions that one wavefront adds up
+constexpr int kSmallT = 256;           // positions per agent up to which nothing is sorted
+constexpr int kLdsT = 16384;           // ... up to which one workgroup sorts them in LDS
+constexpr int kTile = 4096;            // positions per workgroup where several sort together
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+struct EmbedGradPlan {
+  bool small, lds;
+  int32_t bits, pos_bits, chunks, tiles;
+  int64_t pitch;                       // floats per partial sum
+  int64_t tok0, pos0, tok1, pos1, hist, partial, bytes;   // offsets in the workspace
+};
+inline int bits_of(uint32_t v) { return v ? 32 - __builtin_clz(v) : 0; }
+inline EmbedGradPlan plan_embed_grad(int64_t n, int64_t V, int64_t h, int64_t T) {
+  EmbedGradPlan p{};
+  p.small = T <= kSmallT;
+  if (p.small) return p;
+  p.bits = bits_of((uint32_t)V);       // V itself stands for padding
+  p.pos_bits = bits_of((uint32_t)(T - 1));
+  p.lds = T <= kLdsT && p.bits + p.pos_bits <= 32;
+  p.chunks = (int32_t)((T + kChunk - 1) / kChunk);
+  p.tiles = p.lds ? 1 : (int32_t)((T + kTile - 1) / kTile);
+  p.pitch = (h + 3) / 4 * 4;
+  auto take = [&](int64_t bytes) { const int64_t at = p.bytes; p.bytes += (bytes + 255) / 256 * 256; return at; };
+  p.tok0 = take(n * T * 4);
+  p.pos0 = take(n * T * 4);
+  if (!p.lds) {
+    p.tok1 = take(n * T * 4);
+    p.pos1 = take(n * T * 4);
+    p.hist = take(n * p.tiles * (int64_t)kDigits * 4);
+  }
+  p.partial = take(n * p.chunks * 2 * p.pitch * 4);
+  return p;
+}
 
 struct DistillArgs {
   const void* logits;

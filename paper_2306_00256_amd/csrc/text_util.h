@@ -24,4 +24,21 @@ template <> __device__ __forceinline__ bf16_t from_float<bf16_t>(float v) {
   return bf16_t{__builtin_bit_cast(uint16_t, b)};
 }
 
+// VEC neighbouring elements of a row.  Rows may begin at any element, so the access claims no more than an element's alignment
+// (a 16-byte load or store of this chip needs no more).
+template <typename T> struct RawOf { using R = T; };
+template <> struct RawOf<bf16_t> { using R = uint16_t; };
+template <typename T, int VEC> struct Pack {
+  using R = typename RawOf<T>::R;
+  typedef R Mem __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
+  typedef R Reg __attribute__((ext_vector_type(VEC)));
+  Reg v;
+  __device__ __forceinline__ static Pack load(const T* p) { return Pack{*reinterpret_cast<const Mem*>(p)}; }
+  __device__ __forceinline__ static Pack load_stream(const T* p) { return Pack{__builtin_nontemporal_load(reinterpret_cast<const Mem*>(p))}; }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Mem*>(p) = v; }
+  __device__ __forceinline__ void store_stream(T* p) const { __builtin_nontemporal_store((Mem)v, reinterpret_cast<Mem*>(p)); }
+  __device__ __forceinline__ float get(int k) const { return to_float(__builtin_bit_cast(T, (R)v[k])); }
+  __device__ __forceinline__ void set(int k, float x) { v[k] = __builtin_bit_cast(R, from_float<T>(x)); }
+};
+
 }  // namespace ceca
