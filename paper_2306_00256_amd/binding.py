@@ -267,63 +267,81 @@ def _refuse(msg: str):
     raise CecaError(CECA_EINVAL, msg)
 
 
+_torch = None
+_ELEM = {}
+
+
 def _elem_type(name: str, t) -> int:
-    import torch
-    code = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}.get(t.dtype)
+    if not _ELEM:
+        import torch
+        _ELEM.update({torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16})
+    code = _ELEM.get(t.dtype)
     return _refuse(f"{name} is {t.dtype}: float32, bfloat16 or float16 needed") if code is None else code
 
 
 def _rows_pitch(name: str, t, rows: int, width: int) -> int:
     """The pitch of a tensor that holds `rows` rows of `width` contiguous elements, whatever its leading dimensions."""
-    if t.dim() < 1 or t.shape[-1] != width or t.numel() != rows * width:
-        _refuse(f"{name} has the shape {tuple(t.shape)}: {rows} rows of {width} needed")
-    if width > 1 and t.stride(-1) != 1:
-        _refuse(f"{name}: the elements of a row have to be contiguous")
-    if rows == 0:
+    shape = t.shape
+    if not shape or shape[-1] != width or t.numel() != rows * width:
+        _refuse(f"{name} has the shape {tuple(shape)}: {rows} rows of {width} needed")
+    if rows == 0 or t.is_contiguous():
         return width
+    stride = t.stride()
+    if width > 1 and stride[-1] != 1:
+        _refuse(f"{name}: the elements of a row have to be contiguous")
     pitch, inner = None, 1
-    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
-        if size != 1:
+    for k in range(len(shape) - 2, -1, -1):
+        if shape[k] != 1:
             if pitch is None:
-                pitch = stride
-            elif stride != pitch * inner:
+                pitch = stride[k]
+            elif stride[k] != pitch * inner:
                 _refuse(f"{name}: its rows have to lie at one pitch")
-            inner *= size
-    return width if pitch is None else int(pitch)
+            inner *= shape[k]
+    return width if pitch is None else pitch
 
 
 def _flat(name: str, t, dtype: str, count: int) -> None:
-    if str(t.dtype) != "torch." + dtype or t.numel() != count or not t.is_contiguous():
+    if str(t.dtype) != dtype or t.numel() != count or not t.is_contiguous():
         _refuse(f"{name}: {count} contiguous elements of {dtype} needed, not {tuple(t.shape)} of {t.dtype}")
 
 
-def _on_device(stream, *tensors) -> None:
-    """Kernels run on the current device: tensors and stream have to be its own."""
-    import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            _refuse(f"a tensor on {t.device}: the current device's memory (cuda:{dev}) is needed")
-    if stream is not None and stream.device.index != dev:
-        _refuse(f"a stream of {stream.device}: the current device is cuda:{dev}")
+def _stream_of(stream, first, *others) -> Optional[int]:
+    """The stream's handle.  Kernels run on the current device: the tensors and the stream have to be its own."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            _refuse(f"tensors on {first.device} and {t.device}: one device's memory is needed")
+    if dev < 0 or dev != _torch.cuda.current_device():
+        _refuse(f"a tensor on {first.device}: the current device's memory is needed")
+    if stream is None:
+        return _torch._C._cuda_getCurrentRawStream(dev) or None        # current_stream() without its object
+    if stream.device.index != dev:
+        _refuse(f"a stream of {stream.device}, and tensors on {first.device}")
+    return int(stream.cuda_stream) or None
 
 
 def _tables(E, n: int, V: int, h: int):
     """(lde, ldr) of the agents' tables: E of n rows that begin with V rows of h floats each, or of the shape (n, V, h)."""
-    if str(E.dtype) != "torch.float32":
+    if _elem_type("E", E) != TYPE_F32:
         _refuse(f"E is {E.dtype}: float32 needed")
-    if E.dim() == 3 and tuple(E.shape) == (n, V, h) and (h == 1 or E.stride(2) == 1):
-        return int(E.stride(0)), int(E.stride(1)) if V > 1 else max(h, int(E.stride(1)))
-    if E.dim() == 2 and E.shape[0] == n and E.shape[1] >= V * h and (E.shape[1] == 1 or E.stride(1) == 1):
-        return int(E.stride(0)), h
-    return _refuse(f"E has the shape {tuple(E.shape)} and the strides {tuple(E.stride())}: ({n}, {V}, {h}) or {n} rows of at least {V * h} needed, rows contiguous")
+    shape, stride = E.shape, E.stride()
+    if len(shape) == 2 and shape[0] == n and shape[1] >= V * h and (shape[1] == 1 or stride[1] == 1):
+        return stride[0], h
+    if len(shape) == 3 and shape == (n, V, h) and (h == 1 or stride[2] == 1):
+        return stride[0], stride[1] if V > 1 else h
+    return _refuse(f"E has the shape {tuple(shape)} and the strides {stride}: ({n}, {V}, {h}) or {n} rows of at least {V * h} needed, rows contiguous")
 
 
 def _positions(tokens, n: int) -> int:
-    if n < 1 or tokens.numel() % n:
-        _refuse(f"{tokens.numel()} tokens are no whole number for each of n = {n} agents")
-    _flat("tokens", tokens, "int32", tokens.numel())
-    return tokens.numel() // n
+    count = tokens.numel()
+    if n < 1 or count % n:
+        _refuse(f"{count} tokens are no whole number for each of n = {n} agents")
+    _flat("tokens", tokens, "torch.int32", count)
+    return count // n
 
 
 def _workspace_bytes(workspace) -> int:
@@ -340,8 +358,8 @@ def ceca_embed(E, n: int, V: int, h: int, tokens, out, scale: float = 1.0, strea
     T = _positions(tokens, n)
     lde, ldr = _tables(E, n, V, h)
     ldo = _rows_pitch("out", out, n * T, h)
-    _on_device(stream, E, tokens, out)
-    _check(lib().ceca_embed(_ptr(E), lde, ldr, n, V, h, _ptr(tokens), T, scale, _ptr(out), _elem_type("out", out), ldo, _stream(stream)))
+    st = _stream_of(stream, E, tokens, out)
+    _check(lib().ceca_embed(E.data_ptr(), lde, ldr, n, V, h, tokens.data_ptr(), T, scale, out.data_ptr(), _elem_type("out", out), ldo, st))
 
 
 def ceca_embed_grad_workspace_bytes(n: int, T: int, V: int, h: int) -> int:
@@ -353,9 +371,9 @@ def ceca_embed_grad(G, n: int, V: int, h: int, tokens, E, scale: float = 1.0, ac
     T = _positions(tokens, n)
     lde, ldr = _tables(E, n, V, h)
     ldg = _rows_pitch("G", G, n * T, h)
-    _on_device(stream, G, tokens, E, workspace)
-    _check(lib().ceca_embed_grad(_ptr(G), _elem_type("G", G), ldg, _ptr(tokens), T, scale, int(accumulate), _ptr(E), lde, ldr, n, V, h,
-                                 _ptr(workspace), _workspace_bytes(workspace), _stream(stream)))
+    st = _stream_of(stream, E, G, tokens, workspace)
+    _check(lib().ceca_embed_grad(G.data_ptr(), _elem_type("G", G), ldg, tokens.data_ptr(), T, scale, int(accumulate), E.data_ptr(), lde, ldr, n, V, h,
+                                 _ptr(workspace), _workspace_bytes(workspace), st))
 
 
 def make_distill(logits, n: int, T: int, V: int, top=None, ids=None, peer=None, labels=None, weight=None, temperature: float = 1.0,
@@ -369,9 +387,9 @@ def make_distill(logits, n: int, T: int, V: int, top=None, ids=None, peer=None, 
     K = 0
     if top is not None:
         K = int(top.shape[-1]) if top.dim() else 0
-        _flat("top", top, "float32", n * T * K)
-        _flat("ids", ids, "int32", n * T * K)
-    for name, t, dtype, count in (("peer", peer, "int32", n), ("labels", labels, "int32", n * T), ("weight", weight, "float32", n * T)):
+        _flat("top", top, "torch.float32", n * T * K)
+        _flat("ids", ids, "torch.int32", n * T * K)
+    for name, t, dtype, count in (("peer", peer, "torch.int32", n), ("labels", labels, "torch.int32", n * T), ("weight", weight, "torch.float32", n * T)):
         if t is not None:
             _flat(name, t, dtype, count)
     spec = Distill(n=n, T=T, V=V, K=K, type=_elem_type("logits", logits), temperature=temperature, hard=hard, logits=_ptr(logits),
@@ -389,13 +407,15 @@ def ceca_distill(spec: Distill, loss=None, grad=None, workspace=None, stream=Non
     """loss: n x T float32, or None; grad: n x T rows of V of the logits' type (or the logits themselves), or None."""
     ldg = 0
     if loss is not None:
-        _flat("loss", loss, "float32", spec.n * spec.T)
+        _flat("loss", loss, "torch.float32", spec.n * spec.T)
     if grad is not None:
         if _elem_type("grad", grad) != spec.type:
             _refuse(f"grad is {grad.dtype}: the logits' type is needed")
         ldg = _rows_pitch("grad", grad, spec.n * spec.T, spec.V)
-    _on_device(stream, loss, grad, workspace, *getattr(spec, "tensors", ()))
-    _check(lib().ceca_distill(C.byref(spec), _ptr(loss), _ptr(grad), ldg, _ptr(workspace), _workspace_bytes(workspace), _stream(stream)))
+    if loss is None and grad is None:
+        _refuse("neither loss nor gradient asked for")
+    st = _stream_of(stream, grad if loss is None else loss, grad, workspace, *getattr(spec, "tensors", ()))
+    _check(lib().ceca_distill(C.byref(spec), _ptr(loss), _ptr(grad), ldg, _ptr(workspace), _workspace_bytes(workspace), st))
 
 
 def ceca_top_logits_workspace_bytes(logits, rows: int, V: int, K: int) -> int:
@@ -405,11 +425,11 @@ def ceca_top_logits_workspace_bytes(logits, rows: int, V: int, K: int) -> int:
 def ceca_top_logits(logits, rows: int, V: int, K: int, top, ids, workspace=None, stream=None) -> None:
     """The K largest logits of every row and their places (top: float32, ids: int32, rows x K), from the largest down."""
     ld = _rows_pitch("logits", logits, rows, V)
-    _flat("top", top, "float32", rows * K)
-    _flat("ids", ids, "int32", rows * K)
-    _on_device(stream, logits, top, ids, workspace)
-    _check(lib().ceca_top_logits(_ptr(logits), _elem_type("logits", logits), ld, rows, V, K, _ptr(top), _ptr(ids), _ptr(workspace),
-                                 _workspace_bytes(workspace), _stream(stream)))
+    _flat("top", top, "torch.float32", rows * K)
+    _flat("ids", ids, "torch.int32", rows * K)
+    st = _stream_of(stream, logits, top, ids, workspace)
+    _check(lib().ceca_top_logits(logits.data_ptr(), _elem_type("logits", logits), ld, rows, V, K, top.data_ptr(), ids.data_ptr(), _ptr(workspace),
+                                 _workspace_bytes(workspace), st))
 
 
 def consensus_error_workspace_bytes(n: int, d: int) -> int:
