@@ -613,8 +613,8 @@ int64_t elem_size(int32_t type) { return type == CECA_F32 ? 4 : 2; }
 bool on_elements(const void* p, int64_t size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) == 0; }
 
 // Bytes from the first to the last element of `rows` rows of `width` elements, `pitch` apart; 0 without rows.
-// (More than 2^47 bytes lie beyond any device's memory; the product must not overflow.)
-constexpr int64_t kMostBytes = 1LL << 47;
+// (2^43 bytes lie beyond any device's memory; the product must not overflow, and kernels count blocks of 4 KB in 32 bits.)
+constexpr int64_t kMostBytes = 1LL << 43;
 constexpr int32_t kMostColumns = 1 << 30;      // kernels count columns in 32 bits, past the end of a row by a tile
 bool span_bytes(int64_t rows, int64_t pitch, int64_t width, int64_t size, int64_t* bytes) {
   *bytes = 0;

@@ -8,51 +8,86 @@ namespace ceca {
 
 namespace {
 
-// out[i, t, :] = scale * E_i[token, :], one wavefront per position; zeros where the token is none of the vocabulary.
-template <typename T>
-__global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
-  const int64_t rows = (int64_t)a.n * a.T;
-  for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < rows; row += (int64_t)gridDim.x * 4) {
-    const int32_t token = a.tokens[row];
-    const bool real = token >= 0 && token < a.V;
-    const float* e = a.E + row / a.T * a.lde + (real ? token : 0) * a.ldr;
-    T* out = static_cast<T*>(a.rows) + row * a.ldo;
-    for (int32_t c = threadIdx.x % 64; c < a.h; c += 64) out[c] = from_float<T>(real ? a.scale * e[c] : 0.0f);
+// A lane's columns of one row: VEC of them from column c on, the last VEC where fewer are left (it stores its own alone).
+template <int VEC> struct Columns {
+  int32_t c, at;              // first own column, first column read
+  bool whole, some;
+  __device__ __forceinline__ Columns(int32_t first, int32_t h) : c(first), at(min(first, h - VEC)), whole(first + VEC <= h), some(first < h) {}
+  template <typename T> __device__ __forceinline__ void store(T* row, const float (&x)[VEC]) const {
+    Pack<T, VEC> v;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) v.set(k, x[k]);
+    if (whole) {
+      v.store(row + at);
+    } else if (some) {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k)
+        if (at + k >= c) row[at + k] = __builtin_bit_cast(T, (typename Pack<T, VEC>::R)v.v[k]);
+    }
+  }
+};
+
+// out[i, t, :] = scale * E_i[token, :], zeros where the token is none of the vocabulary.  Read and write once; a wavefront has
+// 64 VEC columns of ROWS positions, all loads before the first store.
+template <typename T, int VEC, int ROWS>
+__global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int32_t tiles) {
+  const int64_t rows = (int64_t)a.n * a.T, groups = (rows + ROWS - 1) / ROWS, units = groups * tiles;
+  for (int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); unit < units; unit += (int64_t)gridDim.x * 4) {
+    const int64_t group = unit / tiles, row0 = group * ROWS;
+    const Columns<VEC> col((int32_t)(unit - group * tiles) * 64 * VEC + threadIdx.x % 64 * VEC, a.h);
+    if (!col.some) continue;
+    Pack<float, VEC> e[ROWS];
+    bool real[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const int64_t row = min(row0 + k, rows - 1), i = row / a.T;
+      const int32_t token = a.tokens[row];
+      real[k] = token >= 0 && token < a.V;
+      e[k] = Pack<float, VEC>::load(a.E + i * a.lde + (real[k] ? token : 0) * a.ldr + col.at);
+    }
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      if (row0 + k >= rows) break;
+      float x[VEC];
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) x[c] = real[k] ? a.scale * e[k].get(c) : 0.0f;
+      col.store(static_cast<T*>(a.rows) + (row0 + k) * a.ldo, x);
+    }
   }
 }
 
 // ---- the gradient ----
 // e_i[v, :] = scale * sum of G's rows at v's positions.  A position's row is read once, a table's row is written once: what bounds
-// it is the memory's rate, mostly for the zeros of rows whose tokens do not occur.  Three launches:
-//   sort   positions into the order of (token, position), in LDS; the other workgroups of the same launch write the zeros, so
-//          that neither waits for the other
+// it is the memory's rate, mostly for the zeros of rows whose tokens do not occur.  Four launches:
+//   zeros  over the tables (not where the sums are added to what is there)
+//   sort   positions into the order of (token, position), in LDS
 //   walk   a wavefront adds the rows of kChunk sorted positions up, in order; where a token's positions lie in one chunk its row
 //          of the table is done, else the chunk's share goes to the workspace
 //   join   the shares of tokens that lie in several chunks, in their order
-// Which lane adds what follows from the tokens alone: no atomics, the same bits every time.
+// Which lane adds what follows from the tokens alone: no atomics on sums, the same bits every time.
+// Zeros for the rows that no token names alone, by the walk's launch from a byte per row, were slower: 31 tables of 32000 x 512 575 us
+// against 298 + 37 for all zeros and the walk.
 
-// Zeros over `count` floats, by THREADS threads.
-constexpr int64_t kFillFloats = 32768;
-
-template <int THREADS>
-__device__ __forceinline__ void fill_zeros(float* p, int64_t count) {
-  const vf4 zero{0.0f, 0.0f, 0.0f, 0.0f};
-  const int64_t groups = count / 4;
-  for (int64_t g = threadIdx.x; g < groups; g += THREADS) st_stream<vf4>(p + 4 * g, zero);
-  const int64_t c = groups * 4 + threadIdx.x;
-  if (c < count) p[c] = 0.0f;
+// One 16-byte store per thread and short-lived workgroups in the order of memory are the fastest way to write zeros: 2 GB at 6.8
+// TB/s, 6.0 with two stores, 5.6 to 6.1 with four and more or 1024 threads, 4.5 to 5.8 with long-lived workgroups that sweep
+// memory together.  `all` workgroups' shares, `blocks` per piece of `count` floats, `pitch` apart.
+__global__ __launch_bounds__(256) void zeros_kernel(float* p, int64_t count, int64_t pitch, uint32_t blocks, uint32_t all) {
+  for (uint64_t b = blockIdx.x; b < all; b += gridDim.x) {
+    const uint32_t i = blocks == all ? 0 : (uint32_t)b / blocks;
+    const int64_t at = (int64_t)((uint32_t)b - i * blocks) * 1024 + threadIdx.x * 4;
+    float* q = p + i * pitch;
+    if (at + 4 <= count) st_plain<vf4>(q + at, vf4{0.0f, 0.0f, 0.0f, 0.0f});
+    else
+      for (int64_t k = at; k < count; ++k) q[k] = 0.0f;
+  }
 }
-
-// Part `part` of the tables: runs of rows, as one piece where nothing lies between them.
-template <int THREADS>
-__device__ __forceinline__ void fill_part(const EmbedArgs& a, int64_t part, int32_t run, int64_t runs) {
-  const int64_t i = part / runs;
-  const int32_t v0 = (int32_t)(part - i * runs) * run, v1 = (int32_t)min((int64_t)v0 + run, (int64_t)a.V);
-  float* e = a.dE + i * a.lde;
-  if (a.ldr == a.h) {
-    fill_zeros<THREADS>(e + v0 * a.ldr, (int64_t)(v1 - v0) * a.h);
-  } else {
-    for (int32_t v = v0; v < v1; ++v) fill_zeros<THREADS>(e + v * a.ldr, a.h);
+// The same where something lies between the rows: a wavefront per row.
+__global__ __launch_bounds__(256) void zero_rows_kernel(EmbedArgs a) {
+  const int64_t rows = (int64_t)a.n * a.V;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < rows; row += (int64_t)gridDim.x * 4) {
+    const int64_t i = row / a.V;
+    float* q = a.dE + i * a.lde + (row - i * a.V) * a.ldr;
+    for (int32_t c = threadIdx.x % 64; c < a.h; c += 64) q[c] = 0.0f;
   }
 }
 
@@ -109,55 +144,44 @@ __device__ __forceinline__ void rank_keys(const uint32_t (&key)[IPT], uint32_t (
   for (int j = 0; j < IPT; ++j) to[j] += mine[key[j] >> shift & (digits - 1)];
 }
 
-struct SortArgs {
-  EmbedArgs e;
-  EmbedGradPlan p;
-  int32_t run;                // rows per part of the fill
-  int64_t runs, sorts, parts; // parts per table, workgroups that sort, parts in all (0: nothing is filled)
-};
-
 // Agents' positions sorted by one workgroup each: the keys are (token, position) in one word, so that LDS holds up to 16384 of
 // them beside the counts.
 template <int IPT>
-__global__ __launch_bounds__(1024) void sort_lds_kernel(SortArgs s) {
+__global__ __launch_bounds__(1024) void sort_lds_kernel(EmbedArgs a, EmbedGradPlan p) {
   extern __shared__ uint32_t lds[];
-  const EmbedArgs& a = s.e;
-  if ((int64_t)blockIdx.x >= s.sorts) {
-    for (int64_t part = blockIdx.x - s.sorts; part < s.parts; part += gridDim.x - s.sorts) fill_part<1024>(a, part, s.run, s.runs);
-    return;
-  }
   uint32_t* count = lds;                               // 16 x digits
   uint32_t* totals = lds + 16 * kDigits;
   uint32_t* keys = totals + 16;                        // IPT * 1024
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  for (int64_t i = blockIdx.x; i < a.n; i += s.sorts) {
+  for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
     const int32_t* tokens = a.tokens + i * a.T;
     uint32_t key[IPT], to[IPT];
-    const uint32_t none = (uint32_t)((((uint64_t)1 << (s.p.bits + s.p.pos_bits)) - 1));
+    const uint32_t none = (uint32_t)((((uint64_t)1 << (p.bits + p.pos_bits)) - 1));
 #pragma unroll
     for (int j = 0; j < IPT; ++j) {
       const int t = (wave * IPT + j) * 64 + lane;
       const int32_t v = t < a.T ? tokens[t] : -1;
       // places past the last position go last of all: the largest key, and behind the others of it
-      key[j] = t < a.T ? (uint32_t)(v >= 0 && v < a.V ? v : a.V) << s.p.pos_bits | (uint32_t)t : none;
+      const bool real = v >= 0 && v < a.V;
+      key[j] = t < a.T ? (uint32_t)(real ? v : a.V) << p.pos_bits | (uint32_t)t : none;
     }
-    for (int shift = 0; shift < s.p.bits; shift += kDigitBits) {
-      const int bits = min(kDigitBits, s.p.bits - shift);
-      rank_keys<IPT>(key, to, s.p.pos_bits + shift, bits, count, totals);
+    for (int shift = 0; shift < p.bits; shift += p.digit_bits) {
+      const int bits = min(p.digit_bits, p.bits - shift);
+      rank_keys<IPT>(key, to, p.pos_bits + shift, bits, count, totals);
 #pragma unroll
       for (int j = 0; j < IPT; ++j) keys[to[j]] = key[j];
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < IPT; ++j) key[j] = keys[(wave * IPT + j) * 64 + lane];
     }
-    uint32_t* tok = reinterpret_cast<uint32_t*>(static_cast<char*>(a.workspace) + s.p.tok0) + i * a.T;
-    uint32_t* pos = reinterpret_cast<uint32_t*>(static_cast<char*>(a.workspace) + s.p.pos0) + i * a.T;
+    uint32_t* tok = reinterpret_cast<uint32_t*>(static_cast<char*>(a.workspace) + p.tok0) + i * a.T;
+    uint32_t* pos = reinterpret_cast<uint32_t*>(static_cast<char*>(a.workspace) + p.pos0) + i * a.T;
 #pragma unroll
     for (int j = 0; j < IPT; ++j) {
       const int t = (wave * IPT + j) * 64 + lane;
       if (t < a.T) {
-        tok[t] = min(key[j] >> s.p.pos_bits, (uint32_t)a.V);
-        pos[t] = key[j] & (((uint32_t)1 << s.p.pos_bits) - 1);
+        tok[t] = min(key[j] >> p.pos_bits, (uint32_t)a.V);
+        pos[t] = key[j] & (((uint32_t)1 << p.pos_bits) - 1);
       }
     }
     __syncthreads();
@@ -176,14 +200,10 @@ __device__ __forceinline__ uint32_t pass_key(const PassArgs& p, int64_t i, int64
   const int32_t v = p.tokens[i * p.T + t];
   return (uint32_t)(v >= 0 && v < p.V ? v : p.V);
 }
-__global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p, EmbedArgs a, int32_t run, int64_t runs, int64_t part0, int64_t part1) {
+__global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p) {
   __shared__ uint32_t count[kDigits];
   const int64_t sorts = (int64_t)p.n * p.tiles;
-  for (int64_t b = blockIdx.x; b < sorts + part1 - part0; b += gridDim.x) {
-    if (b >= sorts) {
-      fill_part<1024>(a, part0 + b - sorts, run, runs);
-      continue;
-    }
+  for (int64_t b = blockIdx.x; b < sorts; b += gridDim.x) {
     const int64_t i = b / p.tiles, t0 = (b - i * p.tiles) * kTile;
     if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
     __syncthreads();
@@ -195,16 +215,12 @@ __global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p, EmbedArg
   }
 }
 // ... then every tile's keys to their places: behind the smaller digits of all tiles and the same digit's of earlier tiles.
-__global__ __launch_bounds__(1024) void place_keys_kernel(PassArgs p, EmbedArgs a, int32_t run, int64_t runs, int64_t part0, int64_t part1) {
+__global__ __launch_bounds__(1024) void place_keys_kernel(PassArgs p) {
   constexpr int IPT = kTile / 1024;
   __shared__ uint32_t count[16 * kDigits], totals[16], base[kDigits], sums[16];
   const int64_t sorts = (int64_t)p.n * p.tiles;
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  for (int64_t b = blockIdx.x; b < sorts + part1 - part0; b += gridDim.x) {
-    if (b >= sorts) {
-      fill_part<1024>(a, part0 + b - sorts, run, runs);
-      continue;
-    }
+  for (int64_t b = blockIdx.x; b < sorts; b += gridDim.x) {
     const int64_t i = b / p.tiles;
     const int32_t tile = (int32_t)(b - i * p.tiles);
     uint32_t before = 0, all = 0;
@@ -248,24 +264,6 @@ __global__ __launch_bounds__(1024) void place_keys_kernel(PassArgs p, EmbedArgs 
   }
 }
 
-// A lane's columns of one row: VEC of them from column c on, the last VEC where fewer are left (it stores its own alone).
-template <typename T, int VEC> struct Columns {
-  int32_t c, at, h;           // first own column, first column read
-  bool whole, some;
-  __device__ __forceinline__ Columns(int32_t first, int32_t h_) : c(first), at(min(first, h_ - VEC)), h(h_), whole(first + VEC <= h_), some(first < h_) {}
-  __device__ __forceinline__ void store(float* row, const float (&x)[VEC]) const {
-    if (whole) {
-      Pack<float, VEC> v;
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) v.v[k] = x[k];
-      v.store(row + at);
-    } else if (some) {
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) if (at + k >= c) row[at + k] = x[k];
-    }
-  }
-};
-
 struct WalkArgs {
   EmbedArgs e;
   const uint32_t *tok, *pos;
@@ -285,7 +283,7 @@ __global__ __launch_bounds__(256) void walk_kernel(WalkArgs w) {
   for (int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); unit < units; unit += (int64_t)gridDim.x * 4) {
     const int64_t ic = unit / w.tiles, i = ic / w.chunks;
     const int32_t chunk = (int32_t)(ic - i * w.chunks);
-    const Columns<T, VEC> col((int32_t)(unit - ic * w.tiles) * 64 * VEC + lane * VEC, a.h);
+    const Columns<VEC> col((int32_t)(unit - ic * w.tiles) * 64 * VEC + lane * VEC, a.h);
     const T* G = static_cast<const T*>(a.rows) + i * a.T * a.ldo + col.at;
     float* E = a.dE + i * a.lde;
     float* part = w.partial + ic * 2 * w.pitch;
@@ -354,7 +352,7 @@ __global__ __launch_bounds__(256) void join_kernel(WalkArgs w) {
     const uint32_t v = tok[end - 1];
     if (v >= (uint32_t)a.V || tok[end] != v) continue;
     if (chunk > 0 && tok[chunk * kChunk - 1] == v) continue;    // it began earlier
-    const Columns<float, VEC> col((int32_t)(unit - ic * w.tiles) * 64 * VEC + lane * VEC, a.h);
+    const Columns<VEC> col((int32_t)(unit - ic * w.tiles) * 64 * VEC + lane * VEC, a.h);
     const float* part = w.partial + (i * w.chunks + chunk) * 2 * w.pitch;
     float sum[VEC];
     {
@@ -414,7 +412,7 @@ __global__ __launch_bounds__(256) void few_positions_kernel(EmbedArgs a, int32_t
         earlier |= t > k * 64 && (hits[k] & (t - k * 64 >= 64 ? ~0ull : (1ull << (t - k * 64)) - 1)) != 0;
       }
       if (earlier) continue;
-      const Columns<T, VEC> col((rest - t * tiles) * 64 * VEC + lane * VEC, a.h);
+      const Columns<VEC> col((rest - t * tiles) * 64 * VEC + lane * VEC, a.h);
       if (!col.some) continue;
       const T* G = static_cast<const T*>(a.rows) + i * a.T * a.ldo + col.at;
       float* row = a.dE + i * a.lde + (int64_t)v * a.ldr;
@@ -455,22 +453,26 @@ __global__ __launch_bounds__(256) void few_positions_kernel(EmbedArgs a, int32_t
   }
 }
 
-constexpr int64_t kMostBlocks = 1 << 20;
+constexpr int64_t kMostBlocks = 1 << 20, kMostZeros = 15 << 20;    // a launch has fewer than 2^32 threads
 
-template <typename T> struct Lookup {
-  static hipError_t go(const EmbedArgs& a, hipStream_t st) {
-    const int64_t blocks = ((int64_t)a.n * a.T + 3) / 4;
-    embed_kernel<T><<<dim3((uint32_t)std::min(blocks, kMostBlocks)), dim3(256), 0, st>>>(a);
-    return hipGetLastError();
-  }
-};
-
-// Rows per part of the fill: about kFillFloats floats.
+// Rows of about `floats` floats.
 int32_t run_of(const EmbedArgs& a, int64_t floats) { return (int32_t)std::max<int64_t>(std::min<int64_t>(floats / a.h, a.V), 1); }
 uint32_t four_a_block(int64_t units) { return (uint32_t)std::min((units + 3) / 4, kMostBlocks); }
 
+template <typename T, int VEC> hipError_t lookup(const EmbedArgs& a, hipStream_t st) {
+  const int32_t tiles = (a.h + 64 * VEC - 1) / (64 * VEC);
+  const int64_t rows = (int64_t)a.n * a.T;
+  // four positions a wavefront once there are wavefronts enough
+  if (rows * tiles >= 1 << 14) embed_kernel<T, VEC, 4><<<dim3(four_a_block((rows + 3) / 4 * tiles)), dim3(256), 0, st>>>(a, tiles);
+  else embed_kernel<T, VEC, 1><<<dim3(four_a_block(rows * tiles)), dim3(256), 0, st>>>(a, tiles);
+  return hipGetLastError();
+}
+template <typename T> struct Lookup {
+  static hipError_t go(const EmbedArgs& a, hipStream_t st) { return a.h > 128 ? lookup<T, 4>(a, st) : a.h > 64 ? lookup<T, 2>(a, st) : lookup<T, 1>(a, st); }
+};
+
 template <typename T, int VEC, int NT> hipError_t few_positions(const EmbedArgs& a, hipStream_t st) {
-  const int32_t tiles = (a.h + 64 * VEC - 1) / (64 * VEC), run = run_of(a, 4096);
+  const int32_t tiles = (a.h + 64 * VEC - 1) / (64 * VEC), run = run_of(a, 1024);
   const int64_t runs = (a.V + (int64_t)run - 1) / run;
   const int64_t units = (int64_t)a.n * a.T * tiles + (a.accumulate ? 0 : a.n * runs);
   if (units == 0) return hipSuccess;
@@ -479,14 +481,25 @@ template <typename T, int VEC, int NT> hipError_t few_positions(const EmbedArgs&
   return hipGetLastError();
 }
 
-template <int IPT> hipError_t sort_lds(const SortArgs& s, hipStream_t st) {
+hipError_t zeros(const EmbedArgs& a, hipStream_t st) {
+  if (a.ldr != a.h) {
+    zero_rows_kernel<<<dim3(four_a_block((int64_t)a.n * a.V)), dim3(256), 0, st>>>(a);
+    return hipGetLastError();
+  }
+  // one piece where nothing lies between the tables, else one per table; fewer than 2^43 bytes: blocks fit 32 bits
+  const bool whole = a.n == 1 || a.lde == (int64_t)a.V * a.h;
+  const int64_t count = (whole ? a.n : 1) * (int64_t)a.V * a.h, blocks = (count + 1023) / 1024, all = blocks * (whole ? 1 : a.n);
+  zeros_kernel<<<dim3((uint32_t)std::min(all, kMostZeros)), dim3(256), 0, st>>>(a.dE, count, a.lde, (uint32_t)blocks, (uint32_t)all);
+  return hipGetLastError();
+}
+
+template <int IPT> hipError_t sort_lds(const EmbedArgs& a, const EmbedGradPlan& p, hipStream_t st) {
   const size_t lds = (16 * kDigits + 16 + IPT * 1024) * sizeof(uint32_t);
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sort_lds_kernel<IPT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  const int64_t fill = std::min<int64_t>(s.parts, 1 << 16);
-  sort_lds_kernel<IPT><<<dim3((uint32_t)(s.sorts + fill)), dim3(1024), lds, st>>>(s);
+  sort_lds_kernel<IPT><<<dim3((uint32_t)std::min(a.n, 1 << 16)), dim3(1024), lds, st>>>(a, p);
   return hipGetLastError();
 }
 
@@ -494,23 +507,19 @@ template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const Emb
   if (p.small) return a.T <= 64 ? few_positions<T, VEC, 1>(a, st) : few_positions<T, VEC, 4>(a, st);
   char* ws = static_cast<char*>(a.workspace);
   auto words = [&](int64_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
-  SortArgs s{a, p, run_of(a, kFillFloats), 0, std::min<int64_t>(a.n, 1 << 16), 0};
-  s.runs = (a.V + (int64_t)s.run - 1) / s.run;
-  s.parts = a.accumulate ? 0 : a.n * s.runs;
   uint32_t *tok = words(p.tok0), *pos = words(p.pos0);
-  hipError_t e = hipSuccess;
+  hipError_t e = a.accumulate ? hipSuccess : zeros(a, st);
+  if (e != hipSuccess) return e;
   if (p.lds) {
-    e = a.T <= 1024 ? sort_lds<1>(s, st) : a.T <= 2048 ? sort_lds<2>(s, st) : a.T <= 4096 ? sort_lds<4>(s, st) : a.T <= 8192 ? sort_lds<8>(s, st) : sort_lds<16>(s, st);
+    e = a.T <= 1024 ? sort_lds<1>(a, p, st) : a.T <= 2048 ? sort_lds<2>(a, p, st) : a.T <= 4096 ? sort_lds<4>(a, p, st) : a.T <= 8192 ? sort_lds<8>(a, p, st) : sort_lds<16>(a, p, st);
   } else {
-    const int passes = (p.bits + kDigitBits - 1) / kDigitBits;
     uint32_t *tok2 = words(p.tok1), *pos2 = words(p.pos1);
-    for (int k = 0; k < passes && e == hipSuccess; ++k) {
-      PassArgs q{k ? nullptr : a.tokens, tok, pos, tok2, pos2, words(p.hist), a.n, a.V, a.T, p.tiles, k * kDigitBits, std::min(kDigitBits, p.bits - k * kDigitBits)};
-      // the zeros ride in the passes' launches, in equal shares
-      const int64_t cut[3] = {s.parts * (2 * k) / (2 * passes), s.parts * (2 * k + 1) / (2 * passes), s.parts * (2 * k + 2) / (2 * passes)};
-      const int64_t sorts = (int64_t)a.n * p.tiles;
-      count_digits_kernel<<<dim3((uint32_t)std::min(sorts + cut[1] - cut[0], kMostBlocks)), dim3(1024), 0, st>>>(q, a, s.run, s.runs, cut[0], cut[1]);
-      place_keys_kernel<<<dim3((uint32_t)std::min(sorts + cut[2] - cut[1], kMostBlocks)), dim3(1024), 0, st>>>(q, a, s.run, s.runs, cut[1], cut[2]);
+    const dim3 grid((uint32_t)std::min((int64_t)a.n * p.tiles, kMostBlocks));
+    for (int k = 0; k < p.passes && e == hipSuccess; ++k) {
+      const PassArgs q{k ? nullptr : a.tokens, tok, pos, tok2, pos2, words(p.hist), a.n, a.V, a.T, p.tiles, k * p.digit_bits,
+                       std::min(p.digit_bits, p.bits - k * p.digit_bits)};
+      count_digits_kernel<<<grid, dim3(1024), 0, st>>>(q);
+      place_keys_kernel<<<grid, dim3(1024), 0, st>>>(q);
       e = hipGetLastError();
       std::swap(tok, tok2);
       std::swap(pos, pos2);

@@ -33,6 +33,7 @@ constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 struct EmbedGradPlan {
   bool small, lds;
   int32_t bits, pos_bits, chunks, tiles;
+  int32_t passes, digit_bits;          // of the sort
   int64_t pitch;                       // floats per partial sum
   int64_t tok0, pos0, tok1, pos1, hist, partial, bytes;   // offsets in the workspace
 };
@@ -42,6 +43,8 @@ inline EmbedGradPlan plan_embed_grad(int64_t n, int64_t V, int64_t h, int64_t T)
   p.small = T <= kSmallT;
   if (p.small) return p;
   p.bits = bits_of((uint32_t)V);       // V itself stands for padding
+  p.passes = (p.bits + kDigitBits - 1) / kDigitBits;
+  p.digit_bits = (p.bits + p.passes - 1) / p.passes;
   p.pos_bits = bits_of((uint32_t)(T - 1));
   p.lds = T <= kLdsT && p.bits + p.pos_bits <= 32;
   p.chunks = (int32_t)((T + kChunk - 1) / kChunk);
