@@ -360,7 +360,7 @@ int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t*
  *     The type's lowest finite value is an ordinary logit.
  *   - A row with neither term, or with every logit -inf, has loss 0 and a zero gradient.  So has one of weight 0, whose logits
  *     and entries are not looked at (padding may hold anything).
- *   - A NaN or +inf among a row's logits makes its loss and its whole gradient NaN; one among its entries' values its soft
+ *   - Otherwise a NaN or +inf among a row's logits makes its loss and its whole gradient NaN; one among its entries' values its soft
  *     loss and the gradient at its entries' places. */
 #define CECA_TOP_MAX 256
 typedef struct {

@@ -41,12 +41,12 @@ def distill_row(s, u, ids, temperature, hard, label, weight):
     grad = np.zeros(V)
     if weight == 0:
         return 0.0, grad, 0.0
-    if np.isnan(s).any() or np.isposinf(s).any():
-        return np.nan, np.full(V, np.nan), np.nan
     real = [k for k in range(len(ids)) if 0 <= ids[k] < V and not np.isneginf(u[k])]
     soft, labelled = hard < 1 and len(real) > 0, hard > 0 and label is not None and 0 <= label < V
     if np.isneginf(s).all() or not (soft or labelled):
         return 0.0, grad, 0.0
+    if np.isnan(s).any() or np.isposinf(s).any():
+        return np.nan, np.full(V, np.nan), np.nan
     with np.errstate(divide="ignore", invalid="ignore"):
         logq, logr = _log_softmax(s / temperature), _log_softmax(s)
     loss = size = 0.0

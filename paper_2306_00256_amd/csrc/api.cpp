@@ -1429,7 +1429,7 @@ int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t*
   rc = check_workspace(workspace, workspace_bytes, need);
   if (rc != CECA_OK) return rc;
   if (overlaps(E, tb, G, rb) || overlaps(tokens, (int64_t)n * T * 4, E, tb)) return fail(CECA_EINVAL, "E overlaps an input");
-  if (overlaps(workspace, need, G, rb) || overlaps(workspace, need, tokens, (int64_t)n * T * 4) || overlaps(workspace, need, E, tb))
+  if (need > 0 && (overlaps(workspace, need, G, rb) || overlaps(workspace, need, tokens, (int64_t)n * T * 4) || overlaps(workspace, need, E, tb)))
     return fail(CECA_EINVAL, "the workspace overlaps an argument");
   ceca::EmbedArgs a{};
   a.dE = E;  a.lde = lde;  a.ldr = ldr;  a.tokens = tokens;  a.rows = const_cast<void*>(G);  a.ldo = ldg;
@@ -1441,7 +1441,7 @@ int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t*
 int64_t ceca_distill_workspace_bytes(const ceca_distill_t* spec) {
   const int32_t rc = check_distill(spec);
   if (rc != CECA_OK) return rc;
-  return 0;
+  return ceca::plan_distill((int64_t)spec->n * spec->T, spec->V, spec->K, spec->type).bytes;
 }
 
 int32_t ceca_distill(const ceca_distill_t* spec, float* loss, void* grad, int64_t ldg, void* workspace, int64_t workspace_bytes,
@@ -1463,14 +1463,16 @@ int32_t ceca_distill(const ceca_distill_t* spec, float* loss, void* grad, int64_
     const bool itself = b.p == p.logits && grad == p.logits && ldg == p.ld;
     if (grad && !itself && overlaps(grad, gb, b.p, b.bytes)) return fail(CECA_EINVAL, "the gradient overlaps an input");
     if (loss && overlaps(loss, rows * 4, b.p, b.bytes)) return fail(CECA_EINVAL, "the loss overlaps an input");
+    if (need > 0 && overlaps(workspace, need, b.p, b.bytes)) return fail(CECA_EINVAL, "the workspace overlaps an input");
   }
+  if (need > 0 && ((loss && overlaps(workspace, need, loss, rows * 4)) || (grad && overlaps(workspace, need, grad, gb)))) return fail(CECA_EINVAL, "the workspace overlaps an output");
   if (loss && grad && overlaps(loss, rows * 4, grad, gb)) return fail(CECA_EINVAL, "the loss overlaps the gradient");
   const int32_t rc = check_workspace(workspace, workspace_bytes, need);
   if (rc != CECA_OK) return rc;
   ceca::DistillArgs a{};
   a.logits = p.logits;  a.ld = p.ld;  a.grad = grad;  a.ldg = ldg;  a.loss = loss;
   a.top = p.top;  a.ids = p.ids;  a.peer = p.peer;  a.labels = p.hard > 0.0f ? p.labels : nullptr;  a.weight = p.weight;
-  a.n = p.n;  a.T = p.T;  a.V = p.V;  a.K = p.K;  a.type = p.type;  a.tau = p.temperature;  a.hard = p.hard;
+  a.n = p.n;  a.T = p.T;  a.V = p.V;  a.K = p.K;  a.type = p.type;  a.tau = p.temperature;  a.hard = p.hard;  a.workspace = workspace;
   const hipError_t e = ceca::launch_distill(a, (hipStream_t)hip_stream);
   return e == hipSuccess ? CECA_OK : hip_fail(e, "distillation kernel launch");
 }

@@ -1,4 +1,13 @@
 // Distillation from a teacher's top logits: loss and gradient.
+//
+// A row of V student logits s against K teacher entries (u_k, id_k), with tau the temperature, a the share of the hard term and
+// w the row's weight (p = softmax(u / tau), q = softmax(s / tau), r = softmax(s)):
+//   loss = w [(1 - a) tau^2 sum_k p_k (log p_k - log q_id_k) - a log r_label]
+//   dloss / ds_v = w [(1 - a) tau (q_v - sum_{id_k = v} p_k) + a (r_v - [v = label])]
+// What bounds it: the row is read once and its gradient written once; two exponentials per logit (four with two softmaxes) take
+// half as long as the memory at 16 bits per logit, so the loads of one row have to run beside the arithmetic of another.
+#include <algorithm>
+
 #include "device_util.h"
 #include "text_util.h"
 
@@ -9,130 +18,572 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kInf = __builtin_inff();
 
-// Sum and maximum over the workgroup; `red`: one float per wavefront.  fmaxf drops NaN, sums keep it.
-template <int THREADS> __device__ __forceinline__ float block_sum(float v, float* red) {
-  v = wave_sum(v);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
-  __syncthreads();
-  float s = 0.0f;
-  for (int w = 0; w < THREADS / 64; ++w) s += red[w];
-  return s;
+// Over a wavefront's rows of 16 lanes in four steps without LDS, then over the four rows: the same for every lane.
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
-template <int THREADS> __device__ __forceinline__ float block_max(float v, float* red) {
+template <typename F> __device__ __forceinline__ float row_all(float v, F f) {
+  v = f(v, dpp<0xB1>(v));        // lanes 1 apart
+  v = f(v, dpp<0x4E>(v));        // 2
+  v = f(v, dpp<0x141>(v));       // the other four of eight
+  return f(v, dpp<0x140>(v));    // the other eight of sixteen
+}
+__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+template <typename F> __device__ __forceinline__ float wave_all(float v, F f) {
+  v = row_all(v, f);
+  return f(f(lane_value(v, 0), lane_value(v, 16)), f(lane_value(v, 32), lane_value(v, 48)));
+}
+struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };     // drops NaN
+
+// A workgroup's reduction in two halves around a barrier: every wavefront's value to its slot, then all slots (up to 16).
+template <int WAVES, typename F> __device__ __forceinline__ void put(float v, float* slot, F f) {
+  v = wave_all(v, f);
+  if (threadIdx.x % 64 == 0) slot[threadIdx.x / 64] = v;
+}
+template <int WAVES, typename F> __device__ __forceinline__ float take(const float* slot, F f) {
+  float v = slot[0];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
-  __syncthreads();
-  float s = red[0];
-  for (int w = 1; w < THREADS / 64; ++w) s = fmaxf(s, red[w]);
-  return s;
+  for (int k = 1; k < WAVES; ++k) v = f(v, slot[k]);
+  return v;
 }
 
-// One workgroup per row; see ceca.h for the formulas.
-template <typename T>
-__global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
-  __shared__ float red[4], p[kTopMax];
-  __shared__ int32_t id[kTopMax];
-  const int64_t row = blockIdx.x;
-  const int tid = threadIdx.x;
-  const float w = a.weight ? a.weight[row] : 1.0f;
-  T* grad = a.grad ? static_cast<T*>(a.grad) + row * a.ldg : nullptr;
-  if (w == 0.0f) {
-    if (a.loss && tid == 0) a.loss[row] = 0.0f;
-    if (grad) for (int32_t v = tid; v < a.V; v += 256) grad[v] = from_float<T>(0.0f);
-    return;
-  }
-  const T* s = static_cast<const T*>(a.logits) + row * a.ld;
-  // the teacher's entries: shares p of those that are there, id -1 for the others
-  int64_t trow = row;
-  if (a.peer) trow = (int64_t)min(max(a.peer[row / a.T], 0), a.n - 1) * a.T + row % a.T;
-  float u = -kInf;
-  int32_t at = -1;
-  if (tid < a.K) {
-    at = a.ids[trow * a.K + tid];
-    if (at >= 0 && at < a.V) u = a.top[trow * a.K + tid];
-    if (u == -kInf) at = -1;
-  }
-  const float inv_tau = 1.0f / a.tau;
-  float um = block_max<256>(u, red);
-  if (um == -kInf) um = 0.0f;
-  const float ux = (u - um) * inv_tau, ue = expf(ux), usum = block_sum<256>(ue, red);
-  const bool soft = usum != 0.0f && a.hard < 1.0f;
-  const float pk = at >= 0 ? ue / usum : 0.0f, logp = ux - logf(usum);
-  id[tid] = at;
-  p[tid] = pk;
-  const int32_t label = a.labels ? a.labels[row] : -1;
-  const bool hard = a.hard > 0.0f && label >= 0 && label < a.V;
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }       // zero below 2^-126
 
-  // the student's row
-  float m = -kInf;
-  for (int32_t v = tid; v < a.V; v += 256) m = fmaxf(m, to_float(s[v]));
-  m = block_max<256>(m, red);
-  if (m == -kInf) m = 0.0f;
-  float q = 0.0f, r = 0.0f;
-  for (int32_t v = tid; v < a.V; v += 256) {
-    const float x = to_float(s[v]) - m;
-    q += expf(x * inv_tau);
-    r += expf(x);
-  }
-  q = block_sum<256>(q, red);
-  r = block_sum<256>(r, red);
-  const bool empty = r == 0.0f;
-  const float cs = soft && !empty ? w * (1.0f - a.hard) : 0.0f, ch = hard && !empty ? w * a.hard : 0.0f;
+// Columns a thread reads at once: 16 bytes.
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
 
-  float x = 0.0f, term = 0.0f;
-  if (at >= 0) {
-    x = (to_float(s[at]) - m) * inv_tau;
-    if (pk != 0.0f) term = pk * (logp + logf(q) - x);
-  }
-  if (a.loss) {
-    const float sum = block_sum<256>(term, red);
-    if (tid == 0) {
-      float loss = 0.0f;
-      if (cs != 0.0f) loss += cs * a.tau * a.tau * sum;
-      if (ch != 0.0f) loss += ch * (logf(r) - (to_float(s[label]) - m));
-      a.loss[row] = loss;
+// What is known of a row before its logits are: every thread has its entries (EPT of them).
+template <int EPT> struct Entries {
+  float w;
+  int32_t label;
+  int32_t id[EPT];
+  float u[EPT];
+  template <int THREADS> __device__ __forceinline__ void load(const DistillArgs& a, int64_t row) {
+    w = a.weight ? a.weight[row] : 1.0f;
+    label = a.labels ? a.labels[row] : -1;
+    int64_t from = row;
+    if (a.peer) {
+      const int64_t i = row / a.T;
+      from = (int64_t)min(max(a.peer[i], 0), a.n - 1) * a.T + (row - i * a.T);
+    }
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      const int k = e * THREADS + threadIdx.x;
+      id[e] = -1;
+      u[e] = -kInf;
+      if (k < a.K) {
+        id[e] = a.ids[from * a.K + k];
+        u[e] = a.top[from * a.K + k];
+      }
     }
   }
-  if (!grad) return;
-  const float gs = cs * a.tau, qs = cs != 0.0f ? gs / q : 0.0f, rs = ch != 0.0f ? ch / r : 0.0f;
-  const bool zero = cs == 0.0f && ch == 0.0f;
-  __syncthreads();
-  float lx = hard ? to_float(s[label]) - m : 0.0f;        // read before the row is overwritten in place
-  const float sx = at >= 0 ? to_float(s[at]) - m : 0.0f;
-  __syncthreads();
-  for (int32_t v = tid; v < a.V; v += 256) {
-    const float y = to_float(s[v]) - m;
-    grad[v] = from_float<T>(zero ? 0.0f : (cs != 0.0f ? qs * expf(y * inv_tau) : 0.0f) + (ch != 0.0f ? rs * expf(y) : 0.0f));
+  // an id outside the vocabulary or a value of -inf is no entry
+  __device__ __forceinline__ void settle(const DistillArgs& a) {
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      if (id[e] < 0 || id[e] >= a.V) u[e] = -kInf;
+      if (u[e] == -kInf) id[e] = -1;
+    }
+    if (label >= a.V || !(a.hard > 0.0f)) label = -1;
   }
-  // the places of the teacher's entries and of the label once more, with their shares taken off; an id that comes
-  // twice takes both
-  __syncthreads();
-  if (zero) return;
-  if (cs != 0.0f && at >= 0) {
-    float sum = 0.0f;
-    for (int k = 0; k < a.K; ++k) if (id[k] == at) sum += p[k];
-    float g = gs * (expf(sx * inv_tau) / q - sum);
-    if (ch != 0.0f) g += ch * (expf(sx) / r - (at == label ? 1.0f : 0.0f));
-    grad[at] = from_float<T>(g);
+};
+
+// The factors that a row's statistics give: m (the largest logit), q and r (the sums of the exponentials at tau and at 1).
+struct Factors {
+  float cs, ch;        // w (1 - a), w a; zero without the term
+  float gs, qs, rs;    // tau cs, and the factors of the two exponentials in the gradient
+  bool zero;           // neither term, or no logit that is not masked
+  __device__ __forceinline__ Factors(const DistillArgs& a, float w, bool soft, bool labelled, float q, float r) {
+    const bool some = r != 0.0f;
+    cs = soft && some && a.hard < 1.0f ? w * (1.0f - a.hard) : 0.0f;
+    ch = labelled && some ? w * a.hard : 0.0f;
+    zero = !(soft && a.hard < 1.0f) && !labelled;
+    zero = zero || !some;
+    gs = cs * a.tau;
+    qs = cs != 0.0f ? gs / q : 0.0f;
+    rs = ch != 0.0f ? ch / r : 0.0f;
   }
-  if (ch != 0.0f && tid == 0) {
-    bool also = false;
-    for (int k = 0; k < a.K; ++k) also |= cs != 0.0f && id[k] == label;
-    if (!also) grad[label] = from_float<T>((cs != 0.0f ? qs * expf(lx * inv_tau) : 0.0f) + ch * (expf(lx) / r - 1.0f));
+};
+
+// TWO: exponentials at tau and at 1, both terms being asked for at a temperature other than 1; else one factor `k` for all.
+template <bool TWO> struct Scales {
+  float kq, kr;        // log2 e / tau, log2 e
+  __device__ __forceinline__ Scales(const DistillArgs& a) {
+    const bool hard_alone = a.hard >= 1.0f || a.K == 0;
+    kr = kLog2e;
+    kq = !TWO && hard_alone ? kLog2e : kLog2e / a.tau;
   }
+};
+
+template <typename T, bool TWO> __device__ __forceinline__ float gradient_at(float x, const Scales<TWO>& k, const Factors& f) {
+  if (TWO) return __builtin_fmaf(f.qs, exp2_fast(x * k.kq), f.rs * exp2_fast(x * k.kr));
+  return (f.qs + f.rs) * exp2_fast(x * k.kq);
+}
+
+// One entry's part of the loss before its factors: p (log p - log q_id) with x = s_id - m.
+__device__ __forceinline__ float entry_term(float p, float logp, float logq_sum, float x, float inv_tau) {
+  return p != 0.0f ? p * (logp + logq_sum - x * inv_tau) : 0.0f;
+}
+
+// The gradient at an entry's place or at the label, all of it.
+template <bool TWO> __device__ __forceinline__ float gradient_there(float x, float p_sum, bool is_label, const Scales<TWO>& k, const Factors& f, float q, float r) {
+  float g = 0.0f;
+  if (f.cs != 0.0f) g = f.gs * (exp2_fast(x * k.kq) / q - p_sum);
+  if (f.ch != 0.0f) g += f.ch * (exp2_fast(x * (TWO ? k.kr : k.kq)) / r - (is_label ? 1.0f : 0.0f));
+  return g;
+}
+
+// ---- rows that a workgroup holds in registers ----
+// THREADS threads with NP packs of 16 bytes each (and one of the row's last, fewer than a pack's, elements).  While the gradient of
+// a row is computed and stored pack by pack, the next row's packs are loaded into the registers that become free.
+template <typename T, int THREADS, int NP, bool TWO>
+__global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int64_t rows) {
+  constexpr int VEC = kVec<T>, WAVES = THREADS / 64, EPT = THREADS >= kTopMax ? 1 : kTopMax / THREADS;
+  __shared__ float red[6][WAVES], p_of[kTopMax];
+  __shared__ int32_t id_of[kTopMax];
+  const int tid = threadIdx.x;
+  const int32_t packed = a.V / VEC * VEC, tail = a.V - packed;
+  const Scales<TWO> k(a);
+  const float inv_tau = 1.0f / a.tau;
+  // Packs by their 32-bit distance from the row's beginning (a scalar).  One past the row's last holds that one: all threads load,
+  // and what is not there is left out of the sums.  (`mine` is hidden from the compiler in every phase: it would keep all
+  // the distances in registers.)
+  const uint32_t bytes = (uint32_t)packed * sizeof(T), last = bytes ? bytes - 16 : 0;
+  uint32_t mine = tid * 16;
+  auto at = [&](int j) { return mine + (uint32_t)(j * THREADS * 16); };
+  auto there = [&](int j) { return at(j) < bytes; };
+  auto pack_of = [&](int j, const T* s, uint32_t limit) {
+    return Pack<T, VEC>::load_stream(reinterpret_cast<const T*>(reinterpret_cast<const char*>(s) + min(at(j), limit)));
+  };
+  auto logits_of = [&](int64_t row) { return static_cast<const T*>(a.logits) + row * a.ld; };
+  auto grad_of = [&](int64_t row) { return static_cast<T*>(a.grad) + row * a.ldg; };
+  auto blank = [&](int64_t row) {            // loss 0, gradient 0
+    if (a.loss && tid == 0) a.loss[row] = 0.0f;
+    if (!a.grad) return;
+    T* grad = grad_of(row);
+    Pack<T, VEC> z;
+    z.v = 0;
+    for (uint32_t o = tid * 16; o < bytes; o += THREADS * 16) z.store_stream(reinterpret_cast<T*>(reinterpret_cast<char*>(grad) + o));
+    if (tid < tail) grad[packed + tid] = from_float<T>(0.0f);
+  };
+
+  int64_t row = blockIdx.x;
+  Entries<EPT> next;
+  next.template load<THREADS>(a, row);
+  while (row < rows) {
+    if (next.w == 0.0f) {
+      blank(row);
+      row += gridDim.x;
+      if (row < rows) next.template load<THREADS>(a, row);
+      continue;
+    }
+    Pack<T, VEC> x[NP];
+    float xt = -kInf;
+    {
+      const T* s = logits_of(row);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        if (bytes) {
+          x[j] = pack_of(j, s, last);
+        } else {
+#pragma unroll
+          for (int c = 0; c < VEC; ++c) x[j].set(c, -kInf);
+        }
+      }
+      if (tid < tail) xt = to_float(s[packed + tid]);
+    }
+    // a run of rows, each loaded while the one before it is finished
+    bool run = true;
+    while (run) {
+      Entries<EPT> own = next;
+      own.settle(a);
+      const int64_t row1 = row + gridDim.x;
+      const bool more = row1 < rows;
+      const T* s = logits_of(row);
+      // the logits at the entries' places and at the label, before anything is overwritten
+      float se[EPT], sl;
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) se[e] = to_float(s[max(own.id[e], 0)]);
+      sl = to_float(s[max(own.label, 0)]);
+
+      float m = xt, um = -kInf;
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) m = fmaxf(m, x[j].get(c));         // (a pack past the last holds logits of the row: no harm)
+        __builtin_amdgcn_sched_barrier(0);                               // pack by pack: all at once would take twice the registers
+      }
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) um = fmaxf(um, own.u[e]);
+      put<WAVES>(m, red[0], Max());
+      put<WAVES>(um, red[1], Max());
+      __syncthreads();
+      m = take<WAVES>(red[0], Max());
+      um = take<WAVES>(red[1], Max());
+      if (m == -kInf) m = 0.0f;
+      if (um == -kInf) um = 0.0f;
+
+      float q = exp2_fast((xt - m) * k.kq), r = TWO ? exp2_fast((xt - m) * k.kr) : 0.0f, usum = 0.0f, ue[EPT];
+      asm volatile("" : "+v"(mine));
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        float qs = 0.0f, rs = 0.0f;
+        x[j].again();
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) {
+          const float y = x[j].get(c) - m;
+          qs += exp2_fast(y * k.kq);
+          if (TWO) rs += exp2_fast(y * k.kr);
+        }
+        q += there(j) ? qs : 0.0f;
+        if (TWO) r += there(j) ? rs : 0.0f;
+        asm volatile("" : "+v"(q), "+v"(r));               // here and now: put off, the sums would keep all differences
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) {
+        ue[e] = exp2_fast((own.u[e] - um) * inv_tau * kLog2e);
+        usum += ue[e];
+        asm volatile("" ::"v"(se[e]));         // here at the latest: other wavefronts store behind the next barrier
+      }
+      asm volatile("" ::"v"(sl));
+      put<WAVES>(q, red[2], Add());
+      if (TWO) put<WAVES>(r, red[3], Add());
+      put<WAVES>(usum, red[4], Add());
+      __syncthreads();
+      q = take<WAVES>(red[2], Add());
+      r = TWO ? take<WAVES>(red[3], Add()) : q;
+      usum = take<WAVES>(red[4], Add());
+      const Factors f(a, own.w, usum != 0.0f, own.label >= 0, q, r);
+      if (more) next.template load<THREADS>(a, row1);
+      if (f.zero) {
+        blank(row);
+        break;
+      }
+
+      float term = 0.0f, p[EPT];
+      const float lq = logf(q), lu = logf(usum);
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) {
+        p[e] = own.id[e] >= 0 ? ue[e] / usum : 0.0f;
+        if (own.id[e] >= 0) term += entry_term(p[e], (own.u[e] - um) * inv_tau - lu, lq, se[e] - m, inv_tau);
+        if (e * THREADS + tid < a.K) {
+          id_of[e * THREADS + tid] = own.id[e];
+          p_of[e * THREADS + tid] = p[e];
+        }
+      }
+      put<WAVES>(term, red[5], Add());
+      run = a.grad && more && next.w != 0.0f;
+      if (a.grad) {
+        T* grad = grad_of(row);
+        const T* s1 = logits_of(run ? row1 : row);
+        const uint32_t limit = run ? last : 0;            // (else every thread loads the first pack once more)
+        asm volatile("" : "+v"(mine));
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+          x[j].again();
+          if (there(j)) {
+            Pack<T, VEC> g;
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) g.set(c, gradient_at<T, TWO>(x[j].get(c) - m, k, f));
+            g.store_stream(reinterpret_cast<T*>(reinterpret_cast<char*>(grad) + at(j)));
+          }
+          if (bytes) x[j] = pack_of(j, s1, limit);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (tid < tail) {
+          grad[packed + tid] = from_float<T>(gradient_at<T, TWO>(xt - m, k, f));
+          xt = to_float(s1[packed + tid]);
+        }
+      }
+      __syncthreads();
+      if (a.loss && tid == 0) {
+        float loss = 0.0f;
+        if (f.cs != 0.0f) loss += f.cs * a.tau * a.tau * take<WAVES>(red[5], Add());
+        if (f.ch != 0.0f) loss += f.ch * (logf(r) - (sl - m));
+        a.loss[row] = loss;
+      }
+      // the places of the entries and of the label once more, whole: an id that comes twice takes both shares
+      if (a.grad) {
+        T* grad = grad_of(row);
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+          if (f.cs != 0.0f && own.id[e] >= 0) {
+            float sum = 0.0f;
+            for (int j = 0; j < a.K; ++j) sum += id_of[j] == own.id[e] ? p_of[j] : 0.0f;
+            grad[own.id[e]] = from_float<T>(gradient_there<TWO>(se[e] - m, sum, own.id[e] == own.label, k, f, q, r));
+          }
+        }
+        if (f.ch != 0.0f && tid == THREADS - 1) {
+          bool done = false;
+          if (f.cs != 0.0f)
+            for (int j = 0; j < a.K; ++j) done |= id_of[j] == own.label;
+          if (!done) grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
+        }
+      }
+      __syncthreads();                         // red and the entries' arrays are written again
+      if (run) row = row1;
+    }
+    __syncthreads();
+    row += gridDim.x;
+  }
+}
+
+// ---- rows that stream through ----
+// Longer rows than registers hold: a workgroup reads the row twice, the second time mostly from the last-level cache.  Few rows:
+// `parts` workgroups take a row's columns; one launch leaves each part's maximum and sums in the workspace (and the logits at the
+// entries' places, which the gradient may overwrite), a second one joins them and does the rest.
+enum StreamMode : int { STREAM_ALL = 0, STREAM_STATS = 1, STREAM_REST = 2 };
+struct StreamArgs {
+  DistillArgs a;
+  int64_t rows;
+  int32_t parts, cols, mode;
+  float* stats;        // 4 floats per part
+  float* values;       // K + 1 per row
+};
+constexpr int kStreamThreads = 512;
+
+template <typename T, bool TWO>
+__global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamArgs t) {
+  constexpr int VEC = kVec<T>, THREADS = kStreamThreads, WAVES = THREADS / 64, AHEAD = 4;
+  __shared__ float red[6][WAVES], p_of[kTopMax];
+  __shared__ int32_t id_of[kTopMax];
+  const DistillArgs& a = t.a;
+  const int tid = threadIdx.x;
+  const Scales<TWO> k(a);
+  const float inv_tau = 1.0f / a.tau;
+  for (int64_t unit = blockIdx.x; unit < t.rows * t.parts; unit += gridDim.x) {
+    const int64_t row = unit / t.parts;
+    const int32_t part = (int32_t)(unit - row * t.parts), c0 = part * t.cols, c1 = min(c0 + t.cols, a.V);
+    const int32_t packed = c0 + (c1 - c0) / VEC * VEC;       // the rest, fewer than a pack, one by one
+    const T* s = static_cast<const T*>(a.logits) + row * a.ld;
+    T* grad = a.grad ? static_cast<T*>(a.grad) + row * a.ldg : nullptr;
+    Entries<1> own;
+    own.load<THREADS>(a, row);
+    own.settle(a);
+    __syncthreads();                                          // (shared arrays of the unit before)
+    if (own.w == 0.0f) {
+      if (t.mode != STREAM_STATS) {
+        if (a.loss && tid == 0 && part == 0) a.loss[row] = 0.0f;
+        if (grad) {
+          Pack<T, VEC> z;
+          z.v = 0;
+          for (int32_t c = c0 + tid * VEC; c < packed; c += THREADS * VEC) z.store_stream(grad + c);
+          if (packed + tid < c1) grad[packed + tid] = from_float<T>(0.0f);
+        }
+      }
+      continue;
+    }
+    float m = -kInf, q = 0.0f, r = 0.0f;
+    if (t.mode != STREAM_REST) {
+      // running maximum and sums of this thread's columns
+      auto more = [&](float best, auto&& each) {
+        const float m1 = fmaxf(m, best), base = m1 == -kInf ? 0.0f : m1;
+        q *= exp2_fast((m - base) * k.kq);
+        if (TWO) r *= exp2_fast((m - base) * k.kr);
+        each(base);
+        m = m1;
+      };
+      for (int32_t c = c0 + tid * VEC; c < packed; c += THREADS * VEC * AHEAD) {
+        Pack<T, VEC> x[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) x[j] = Pack<T, VEC>::load(s + min(c + j * THREADS * VEC, packed - VEC));
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          if (c + j * THREADS * VEC >= packed) break;
+          float best = x[j].get(0);
+#pragma unroll
+          for (int e = 1; e < VEC; ++e) best = fmaxf(best, x[j].get(e));
+          more(best, [&](float base) {
+            float qs = 0.0f, rs = 0.0f;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              const float y = x[j].get(e) - base;
+              qs += exp2_fast(y * k.kq);
+              if (TWO) rs += exp2_fast(y * k.kr);
+            }
+            q += qs;
+            r += rs;
+          });
+        }
+      }
+      if (packed + tid < c1) {
+        const float y0 = to_float(s[packed + tid]);
+        more(y0, [&](float base) {
+          q += exp2_fast((y0 - base) * k.kq);
+          if (TWO) r += exp2_fast((y0 - base) * k.kr);
+        });
+      }
+      const float mine = m;
+      put<WAVES>(m, red[0], Max());
+      __syncthreads();
+      m = take<WAVES>(red[0], Max());
+      const float base = m == -kInf ? 0.0f : m;
+      q *= exp2_fast((mine - base) * k.kq);
+      if (TWO) r *= exp2_fast((mine - base) * k.kr);
+      put<WAVES>(q, red[2], Add());
+      if (TWO) put<WAVES>(r, red[3], Add());
+      __syncthreads();
+      q = take<WAVES>(red[2], Add());
+      r = TWO ? take<WAVES>(red[3], Add()) : q;
+      if (t.mode == STREAM_STATS) {
+        if (tid == 0) {
+          float* st = t.stats + unit * 4;
+          st[0] = m;
+          st[1] = q;
+          st[2] = r;
+        }
+        // the logits that this part has for the entries and the label
+        float* values = t.values + row * (a.K + 1);
+        if (own.id[0] >= c0 && own.id[0] < c1) values[tid] = to_float(s[own.id[0]]);
+        if (tid == 0 && own.label >= c0 && own.label < c1) values[a.K] = to_float(s[own.label]);
+        continue;
+      }
+    } else {
+      // join the parts: the same order in every workgroup
+      const float* st = t.stats + row * t.parts * 4;
+      for (int32_t j = tid; j < t.parts; j += THREADS) m = fmaxf(m, st[j * 4]);
+      put<WAVES>(m, red[0], Max());
+      __syncthreads();
+      m = take<WAVES>(red[0], Max());
+      const float base = m == -kInf ? 0.0f : m;
+      for (int32_t j = tid; j < t.parts; j += THREADS) {
+        q += st[j * 4 + 1] * exp2_fast((st[j * 4] - base) * k.kq);
+        r += st[j * 4 + 2] * exp2_fast((st[j * 4] - base) * (TWO ? k.kr : k.kq));
+      }
+      put<WAVES>(q, red[2], Add());
+      put<WAVES>(r, red[3], Add());
+      __syncthreads();
+      q = take<WAVES>(red[2], Add());
+      r = take<WAVES>(red[3], Add());
+    }
+    if (m == -kInf) m = 0.0f;
+    float se = 0.0f, sl = 0.0f;
+    if (t.mode == STREAM_REST) {
+      const float* values = t.values + row * (a.K + 1);
+      if (own.id[0] >= 0) se = values[tid];
+      if (own.label >= 0) sl = values[a.K];
+    } else {
+      if (own.id[0] >= 0) se = to_float(s[own.id[0]]);
+      if (own.label >= 0) sl = to_float(s[own.label]);
+      asm volatile("" ::"v"(se), "v"(sl));
+    }
+    float um = own.u[0];
+    put<WAVES>(um, red[1], Max());
+    __syncthreads();
+    um = take<WAVES>(red[1], Max());
+    if (um == -kInf) um = 0.0f;
+    const float ue = exp2_fast((own.u[0] - um) * inv_tau * kLog2e);
+    put<WAVES>(ue, red[4], Add());
+    __syncthreads();
+    const float usum = take<WAVES>(red[4], Add());
+    const Factors f(a, own.w, usum != 0.0f, own.label >= 0, q, r);
+    const float p = own.id[0] >= 0 ? ue / usum : 0.0f;
+    float term = 0.0f;
+    if (own.id[0] >= 0) term = entry_term(p, (own.u[0] - um) * inv_tau - logf(usum), logf(q), se - m, inv_tau);
+    if (tid < a.K) {
+      id_of[tid] = own.id[0];
+      p_of[tid] = p;
+    }
+    put<WAVES>(term, red[5], Add());
+    if (grad) {
+      for (int32_t c = c0 + tid * VEC; c < packed; c += THREADS * VEC * AHEAD) {
+        Pack<T, VEC> x[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) x[j] = Pack<T, VEC>::load(s + min(c + j * THREADS * VEC, packed - VEC));
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          if (c + j * THREADS * VEC >= packed) break;
+          Pack<T, VEC> g;
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) g.set(e, f.zero ? 0.0f : gradient_at<T, TWO>(x[j].get(e) - m, k, f));
+          g.store_stream(grad + c + j * THREADS * VEC);
+        }
+      }
+      if (packed + tid < c1) grad[packed + tid] = from_float<T>(f.zero ? 0.0f : gradient_at<T, TWO>(to_float(s[packed + tid]) - m, k, f));
+    }
+    __syncthreads();
+    if (a.loss && tid == 0 && part == 0) {
+      float loss = 0.0f;
+      if (f.cs != 0.0f) loss += f.cs * a.tau * a.tau * take<WAVES>(red[5], Add());
+      if (f.ch != 0.0f) loss += f.ch * (logf(r) - (sl - m));
+      a.loss[row] = loss;
+    }
+    if (grad && !f.zero) {
+      if (f.cs != 0.0f && own.id[0] >= c0 && own.id[0] < c1) {
+        float sum = 0.0f;
+        for (int j = 0; j < a.K; ++j) sum += id_of[j] == own.id[0] ? p_of[j] : 0.0f;
+        grad[own.id[0]] = from_float<T>(gradient_there<TWO>(se - m, sum, own.id[0] == own.label, k, f, q, r));
+      }
+      if (f.ch != 0.0f && tid == THREADS - 1 && own.label >= c0 && own.label < c1) {
+        bool done = false;
+        if (f.cs != 0.0f)
+          for (int j = 0; j < a.K; ++j) done |= id_of[j] == own.label;
+        if (!done) grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
+      }
+    }
+  }
+}
+
+constexpr int64_t kMostRowBlocks = 1 << 21;       // (a launch has fewer than 2^32 threads)
+
+template <typename T, bool TWO> hipError_t launch(const DistillArgs& a, hipStream_t st) {
+  const int64_t rows = (int64_t)a.n * a.T;
+  const DistillPlan plan = plan_distill(rows, a.V, a.K, a.type);
+  const int32_t packs = a.V / kVec<T>;
+  const uint32_t blocks = (uint32_t)std::min(rows, kMostRowBlocks);
+  if (plan.parts > 1 || packs > 1024 * 16) {
+    StreamArgs t{a, rows, plan.parts, plan.cols, STREAM_ALL, nullptr, nullptr};
+    const dim3 grid((uint32_t)std::min(rows * plan.parts, kMostRowBlocks)), block(kStreamThreads);
+    if (plan.parts > 1) {
+      t.stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.stats);
+      t.values = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.values);
+      t.mode = STREAM_STATS;
+      distill_stream_kernel<T, TWO><<<grid, block, 0, st>>>(t);
+      t.mode = STREAM_REST;
+    }
+    distill_stream_kernel<T, TWO><<<grid, block, 0, st>>>(t);
+    return hipGetLastError();
+  }
+  if (packs <= 64) distill_row_kernel<T, 64, 1, TWO><<<dim3(blocks), dim3(64), 0, st>>>(a, rows);
+  else if (packs <= 64 * 4) distill_row_kernel<T, 64, 4, TWO><<<dim3(blocks), dim3(64), 0, st>>>(a, rows);
+  else if (packs <= 256 * 4) distill_row_kernel<T, 256, 4, TWO><<<dim3(blocks), dim3(256), 0, st>>>(a, rows);
+  else if (packs <= 256 * 8) distill_row_kernel<T, 256, 8, TWO><<<dim3(blocks), dim3(256), 0, st>>>(a, rows);
+  else if (packs <= 256 * 16) distill_row_kernel<T, 256, 16, TWO><<<dim3(blocks), dim3(256), 0, st>>>(a, rows);
+  else if (packs <= 512 * 16) distill_row_kernel<T, 512, 16, TWO><<<dim3(blocks), dim3(512), 0, st>>>(a, rows);
+  else distill_row_kernel<T, 1024, 16, TWO><<<dim3((uint32_t)std::min<int64_t>(rows, 256)), dim3(1024), 0, st>>>(a, rows);
+  return hipGetLastError();
 }
 
 }  // namespace
 
+DistillPlan plan_distill(int64_t rows, int32_t V, int32_t K, int type) {
+  DistillPlan p{};
+  p.parts = 1;
+  p.cols = V;
+  const int32_t vec = type == TYPE_F32 ? 4 : 8;
+  // few rows of many columns: 4096 columns a part or more, up to 512 workgroups
+  if (rows > 0 && rows <= 64 && V >= 32768) {
+    const int32_t most = (int32_t)std::min<int64_t>(V / 4096, 512 / rows);
+    if (most > 1) {
+      p.cols = ((V + most - 1) / most + vec - 1) / vec * vec;
+      p.parts = (V + p.cols - 1) / p.cols;
+    }
+  }
+  if (p.parts > 1) {
+    p.values = (rows * p.parts * 16 + 255) / 256 * 256;
+    p.bytes = p.values + (rows * (K + 1) * 4 + 255) / 256 * 256;
+  }
+  return p;
+}
+
 hipError_t launch_distill(const DistillArgs& a, hipStream_t st) {
-  const dim3 grid((uint32_t)a.n * (uint32_t)a.T), block(256);
-  if (a.type == TYPE_F32) distill_kernel<float><<<grid, block, 0, st>>>(a);
-  else if (a.type == TYPE_BF16) distill_kernel<bf16_t><<<grid, block, 0, st>>>(a);
-  else distill_kernel<_Float16><<<grid, block, 0, st>>>(a);
-  return hipGetLastError();
+  // both terms at a temperature other than 1: two softmaxes
+  const bool two = a.K > 0 && a.hard > 0.0f && a.hard < 1.0f && a.tau != 1.0f;
+  if (a.type == TYPE_F32) return two ? launch<float, true>(a, st) : launch<float, false>(a, st);
+  if (a.type == TYPE_BF16) return two ? launch<bf16_t, true>(a, st) : launch<bf16_t, false>(a, st);
+  return two ? launch<_Float16, true>(a, st) : launch<_Float16, false>(a, st);
 }
 
 }  // namespace ceca

@@ -272,11 +272,16 @@ struct WalkArgs {
   int32_t chunks, tiles;      // chunks per agent, column tiles
 };
 
-constexpr int kAhead = 8;     // rows whose loads are in flight
+// Rows whose loads are in flight: all of a chunk, or four where each may need the table's row too.  Measured, chunks of 16 (walk / join):
+// 31 x 2048 positions of 512 bf16 28 us with 16 ahead, 35 with 8; 6 x 11469 of 1024 fp32 89 with 8 and 16, added to what is there
+// 111 with 4, 120 with 8, 127 with 16.  Chunks of 32 with 8 ahead 45, 98 and 139, joins 5 us shorter; of 8 33, 87 and 112, joins 8
+// longer.
+constexpr int ahead(bool add) { return add ? 4 : kChunk; }
 
 // One wavefront per chunk of sorted positions and tile of 64 VEC columns.
 template <typename T, int VEC, bool ADD>
 __global__ __launch_bounds__(256) void walk_kernel(WalkArgs w) {
+  constexpr int kAhead = ahead(ADD);
   const EmbedArgs& a = w.e;
   const int lane = threadIdx.x % 64;
   const int64_t units = (int64_t)a.n * w.chunks * w.tiles;
@@ -364,6 +369,7 @@ __global__ __launch_bounds__(256) void join_kernel(WalkArgs w) {
       // chunks that begin with the token: a run of them, its end by ballot
       const uint64_t mine = __ballot(c + lane < w.chunks && tok[(int64_t)min(c + lane, w.chunks - 1) * kChunk] == v);
       const int32_t run = mine == ~0ull ? 64 : __builtin_ctzll(~mine);
+      constexpr int kAhead = 8;
       for (int32_t k0 = 0; k0 < run; k0 += kAhead) {
         Pack<float, VEC> p[kAhead];
 #pragma unroll

@@ -25,7 +25,7 @@ struct EmbedArgs {
 };
 
 // How the gradient's positions are brought into the order of their tokens, and its workspace.
-constexpr int kChunk = 32;             // sorted positions that one wavefront adds up
+constexpr int kChunk = 16;             // sorted positions that one wavefront adds up
 constexpr int kSmallT = 256;           // positions per agent up to which nothing is sorted
 constexpr int kLdsT = 16384;           // ... up to which one workgroup sorts them in LDS
 constexpr int kTile = 4096;            // positions per workgroup where several sort together
@@ -76,7 +76,15 @@ struct DistillArgs {
   int32_t n, T, V, K;
   int32_t type;
   float tau, hard;
+  void* workspace;         // of plan_distill(...).bytes
 };
+
+// Rows are split over `parts` workgroups of `cols` columns where there are too few to fill the device.
+struct DistillPlan {
+  int32_t parts, cols;
+  int64_t stats, values, bytes;    // offsets in the workspace
+};
+DistillPlan plan_distill(int64_t rows, int32_t V, int32_t K, int type);
 
 struct TopArgs {
   const void* logits;

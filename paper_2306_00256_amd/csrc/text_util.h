@@ -37,6 +37,15 @@ template <typename T, int VEC> struct Pack {
   __device__ __forceinline__ static Pack load_stream(const T* p) { return Pack{__builtin_nontemporal_load(reinterpret_cast<const Mem*>(p))}; }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Mem*>(p) = v; }
   __device__ __forceinline__ void store_stream(T* p) const { __builtin_nontemporal_store((Mem)v, reinterpret_cast<Mem*>(p)); }
+  // The compiler must work out again what it made of these elements before: kept, the floats of a register tile would take up to twice
+  // the tile's registers.
+  __device__ __forceinline__ void again() {
+    static_assert(sizeof(Reg) == 16, "one 16-byte register tuple");
+    typedef uint32_t U __attribute__((ext_vector_type(4)));
+    U u = __builtin_bit_cast(U, v);
+    asm volatile("" : "+v"(u));
+    v = __builtin_bit_cast(Reg, u);
+  }
   __device__ __forceinline__ float get(int k) const { return to_float(__builtin_bit_cast(T, (R)v[k])); }
   __device__ __forceinline__ void set(int k, float x) { v[k] = __builtin_bit_cast(R, from_float<T>(x)); }
 };
