@@ -36,18 +36,6 @@ template <typename F> __device__ __forceinline__ float wave_all(float v, F f) {
 struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };     // drops NaN
 
-// A workgroup's reduction in two halves around a barrier: every wavefront's value to its slot, then all slots (up to 16).
-template <int WAVES, typename F> __device__ __forceinline__ void put(float v, float* slot, F f) {
-  v = wave_all(v, f);
-  if (threadIdx.x % 64 == 0) slot[threadIdx.x / 64] = v;
-}
-template <int WAVES, typename F> __device__ __forceinline__ float take(const float* slot, F f) {
-  float v = slot[0];
-#pragma unroll
-  for (int k = 1; k < WAVES; ++k) v = f(v, slot[k]);
-  return v;
-}
-
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }       // zero below 2^-126
 
 // Columns a thread reads at once: 16 bytes.
@@ -92,7 +80,7 @@ template <int EPT> struct Entries {
 // The factors that a row's statistics give: m (the largest logit), q and r (the sums of the exponentials at tau and at 1).
 struct Factors {
   float cs, ch;        // w (1 - a), w a; zero without the term
-  float gs, qs, rs;    // tau cs, and the factors of the two exponentials in the gradient
+  float gs, qs, rs, both;    // tau cs, the factors of the two exponentials in the gradient, their sum
   bool zero;           // neither term, or no logit that is not masked
   __device__ __forceinline__ Factors(const DistillArgs& a, float w, bool soft, bool labelled, float q, float r) {
     const bool some = r != 0.0f;
@@ -103,6 +91,8 @@ struct Factors {
     gs = cs * a.tau;
     qs = cs != 0.0f ? gs / q : 0.0f;
     rs = ch != 0.0f ? ch / r : 0.0f;
+    both = qs + rs;
+    asm("" : "+v"(qs), "+v"(rs), "+v"(both));      // (plain arithmetic issues faster without scalar operands)
   }
 };
 
@@ -111,14 +101,14 @@ template <bool TWO> struct Scales {
   float kq, kr;        // log2 e / tau, log2 e
   __device__ __forceinline__ Scales(const DistillArgs& a) {
     const bool hard_alone = a.hard >= 1.0f || a.K == 0;
-    kr = kLog2e;
-    kq = !TWO && hard_alone ? kLog2e : kLog2e / a.tau;
+    kr = in_vgpr(kLog2e);
+    kq = in_vgpr(!TWO && hard_alone ? kLog2e : kLog2e / a.tau);
   }
 };
 
 template <typename T, bool TWO> __device__ __forceinline__ float gradient_at(float x, const Scales<TWO>& k, const Factors& f) {
   if (TWO) return __builtin_fmaf(f.qs, exp2_fast(x * k.kq), f.rs * exp2_fast(x * k.kr));
-  return (f.qs + f.rs) * exp2_fast(x * k.kq);
+  return f.both * exp2_fast(x * k.kq);
 }
 
 // One entry's part of the loss before its factors: p (log p - log q_id) with x = s_id - m.
@@ -134,13 +124,78 @@ template <bool TWO> __device__ __forceinline__ float gradient_there(float x, flo
   return g;
 }
 
+// Running statistics of one thread's logits: their maximum and the sums of the exponentials relative to it.  The lowest finite
+// number stands for "none yet": nothing but masked logits leaves sums of zero behind.
+constexpr float kLowest = -3.402823466e38f;
+template <bool TWO> struct Running {
+  float m = kLowest, q = 0.0f, r = 0.0f;
+  __device__ __forceinline__ void rise(float to, const Scales<TWO>& k) {
+    const float m1 = fmaxf(m, to);
+    q *= exp2_fast((m - m1) * k.kq);
+    if (TWO) r *= exp2_fast((m - m1) * k.kr);
+    m = m1;
+  }
+  __device__ __forceinline__ void add(float x, const Scales<TWO>& k) {
+    rise(x, k);
+    q += exp2_fast((x - m) * k.kq);
+    if (TWO) r += exp2_fast((x - m) * k.kr);
+  }
+  // a pack, counted where `there` (its maximum may count anyway); with `risen` the maximum is known to be no less than its own
+  template <typename P, int VEC> __device__ __forceinline__ void add(const P& x, bool there, const Scales<TWO>& k, bool risen = false) {
+    if (!risen) {
+      float best = x.get(0);
+#pragma unroll
+      for (int c = 1; c < VEC; ++c) best = fmaxf(best, x.get(c));
+      rise(best, k);
+    }
+    float qs = 0.0f, rs = 0.0f;
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) {
+      const float y = x.get(c) - m;
+      qs += exp2_fast(y * k.kq);
+      if (TWO) rs += exp2_fast(y * k.kr);
+    }
+    q += there ? qs : 0.0f;
+    if (TWO) r += there ? rs : 0.0f;
+    asm volatile("" : "+v"(q), "+v"(r));                 // here and now: put off, the sums would keep all differences
+  }
+  __device__ __forceinline__ void over_wave(const Scales<TWO>& k) {
+    rise(wave_all(m, Max()), k);
+    q = wave_all(q, Add());
+    if (TWO) r = wave_all(r, Add());
+  }
+  // slot[0..2]: a float per wavefront each (put before a barrier)
+  __device__ __forceinline__ void put(float (*slot)[16]) const {
+    if (threadIdx.x % 64 == 0) {
+      slot[0][threadIdx.x / 64] = m;
+      slot[1][threadIdx.x / 64] = q;
+      if (TWO) slot[2][threadIdx.x / 64] = r;
+    }
+  }
+  template <int WAVES> __device__ __forceinline__ void take(const float (*slot)[16], const Scales<TWO>& k) {
+    const int w = threadIdx.x % 16;
+    const bool is = w < WAVES;
+    m = is ? slot[0][w] : kLowest;
+    q = is ? slot[1][w] : 0.0f;
+    r = TWO && is ? slot[2][w] : 0.0f;
+    rise(row_all(m, Max()), k);
+    // lane 0's for all: a lane's own product may be fused into its first addition, which rounds differently
+    m = lane_value(m, 0);
+    q = lane_value(row_all(q, Add()), 0);
+    r = TWO ? lane_value(row_all(r, Add()), 0) : q;
+  }
+};
+
 // ---- rows that a workgroup holds in registers ----
-// THREADS threads with NP packs of 16 bytes each (and one of the row's last, fewer than a pack's, elements).  While the gradient of
-// a row is computed and stored pack by pack, the next row's packs are loaded into the registers that become free.
-template <typename T, int THREADS, int NP, bool TWO>
-__global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int64_t rows) {
+// THREADS threads with NP packs of 16 bytes each (and one of the row's last, fewer than a pack's, elements).  LOOP: the workgroup goes
+// on to other rows; while the gradient of one is computed and stored pack by pack, the next row's packs are loaded into the
+// registers that become free and their statistics taken kLag packs later, so that memory is busy all the time.
+constexpr int kLag = 4;
+template <typename T, int THREADS, int NP, bool TWO, bool GRAD, bool LOOP>
+__global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void distill_row_kernel(DistillArgs a, int64_t rows) {
   constexpr int VEC = kVec<T>, WAVES = THREADS / 64, EPT = THREADS >= kTopMax ? 1 : kTopMax / THREADS;
-  __shared__ float red[6][WAVES], p_of[kTopMax];
+  using P = Pack<T, VEC>;
+  __shared__ float red[2][6][16], p_of[kTopMax];         // (two sets in turn: a row's are read behind its barrier)
   __shared__ int32_t id_of[kTopMax];
   const int tid = threadIdx.x;
   const int32_t packed = a.V / VEC * VEC, tail = a.V - packed;
@@ -154,15 +209,15 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
   auto at = [&](int j) { return mine + (uint32_t)(j * THREADS * 16); };
   auto there = [&](int j) { return at(j) < bytes; };
   auto pack_of = [&](int j, const T* s, uint32_t limit) {
-    return Pack<T, VEC>::load_stream(reinterpret_cast<const T*>(reinterpret_cast<const char*>(s) + min(at(j), limit)));
+    return P::load_stream(reinterpret_cast<const T*>(reinterpret_cast<const char*>(s) + min(at(j), limit)));
   };
   auto logits_of = [&](int64_t row) { return static_cast<const T*>(a.logits) + row * a.ld; };
   auto grad_of = [&](int64_t row) { return static_cast<T*>(a.grad) + row * a.ldg; };
   auto blank = [&](int64_t row) {            // loss 0, gradient 0
     if (a.loss && tid == 0) a.loss[row] = 0.0f;
-    if (!a.grad) return;
+    if (!GRAD) return;
     T* grad = grad_of(row);
-    Pack<T, VEC> z;
+    P z;
     z.v = 0;
     for (uint32_t o = tid * 16; o < bytes; o += THREADS * 16) z.store_stream(reinterpret_cast<T*>(reinterpret_cast<char*>(grad) + o));
     if (tid < tail) grad[packed + tid] = from_float<T>(0.0f);
@@ -171,6 +226,7 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
   int64_t row = blockIdx.x;
   Entries<EPT> next;
   next.template load<THREADS>(a, row);
+  int set = 0;
   while (row < rows) {
     if (next.w == 0.0f) {
       blank(row);
@@ -178,7 +234,7 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
       if (row < rows) next.template load<THREADS>(a, row);
       continue;
     }
-    Pack<T, VEC> x[NP];
+    P x[NP];
     float xt = -kInf;
     {
       const T* s = logits_of(row);
@@ -193,7 +249,19 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
       }
       if (tid < tail) xt = to_float(s[packed + tid]);
     }
-    // a run of rows, each loaded while the one before it is finished
+    Running<TWO> st;
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) st.m = fmaxf(st.m, x[j].get(c));
+      __builtin_amdgcn_sched_barrier(0);     // pack by pack: all at once would take twice the registers
+    }
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      x[j].again();
+      st.template add<P, VEC>(x[j], there(j), k, true);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     bool run = true;
     while (run) {
       Entries<EPT> own = next;
@@ -206,106 +274,96 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
 #pragma unroll
       for (int e = 0; e < EPT; ++e) se[e] = to_float(s[max(own.id[e], 0)]);
       sl = to_float(s[max(own.label, 0)]);
+      if (more) next.template load<THREADS>(a, row1);
 
-      float m = xt, um = -kInf;
-#pragma unroll
-      for (int j = 0; j < NP; ++j) {
-#pragma unroll
-        for (int c = 0; c < VEC; ++c) m = fmaxf(m, x[j].get(c));         // (a pack past the last holds logits of the row: no harm)
-        __builtin_amdgcn_sched_barrier(0);                               // pack by pack: all at once would take twice the registers
-      }
+      float um = kLowest, usum = 0.0f, ue[EPT];
 #pragma unroll
       for (int e = 0; e < EPT; ++e) um = fmaxf(um, own.u[e]);
-      put<WAVES>(m, red[0], Max());
-      put<WAVES>(um, red[1], Max());
-      __syncthreads();
-      m = take<WAVES>(red[0], Max());
-      um = take<WAVES>(red[1], Max());
-      if (m == -kInf) m = 0.0f;
-      if (um == -kInf) um = 0.0f;
-
-      float q = exp2_fast((xt - m) * k.kq), r = TWO ? exp2_fast((xt - m) * k.kr) : 0.0f, usum = 0.0f, ue[EPT];
-      asm volatile("" : "+v"(mine));
+      um = wave_all(um, Max());
 #pragma unroll
-      for (int j = 0; j < NP; ++j) {
-        float qs = 0.0f, rs = 0.0f;
-        x[j].again();
-#pragma unroll
-        for (int c = 0; c < VEC; ++c) {
-          const float y = x[j].get(c) - m;
-          qs += exp2_fast(y * k.kq);
-          if (TWO) rs += exp2_fast(y * k.kr);
-        }
-        q += there(j) ? qs : 0.0f;
-        if (TWO) r += there(j) ? rs : 0.0f;
-        asm volatile("" : "+v"(q), "+v"(r));               // here and now: put off, the sums would keep all differences
-        __builtin_amdgcn_sched_barrier(0);
+      for (int e = 0; e < EPT; ++e) usum += exp2_fast((own.u[e] - um) * (inv_tau * kLog2e));
+      usum = wave_all(usum, Add());
+      if (tid < tail) st.add(xt, k);
+      st.over_wave(k);
+      st.put(red[set]);
+      if (tid % 64 == 0) {
+        red[set][3][tid / 64] = um;
+        red[set][4][tid / 64] = usum;
       }
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        ue[e] = exp2_fast((own.u[e] - um) * inv_tau * kLog2e);
-        usum += ue[e];
-        asm volatile("" ::"v"(se[e]));         // here at the latest: other wavefronts store behind the next barrier
-      }
+      for (int e = 0; e < EPT; ++e) asm volatile("" ::"v"(se[e]));        // here at the latest: others store behind the barrier
       asm volatile("" ::"v"(sl));
-      put<WAVES>(q, red[2], Add());
-      if (TWO) put<WAVES>(r, red[3], Add());
-      put<WAVES>(usum, red[4], Add());
       __syncthreads();
-      q = take<WAVES>(red[2], Add());
-      r = TWO ? take<WAVES>(red[3], Add()) : q;
-      usum = take<WAVES>(red[4], Add());
+      st.template take<WAVES>(red[set], k);
+      const float m = in_vgpr(st.m), q = st.q, r = st.r;
+      {
+        const int w = tid % 16;
+        const float mw = w < WAVES ? red[set][3][w] : kLowest, sw = w < WAVES ? red[set][4][w] : 0.0f;
+        um = lane_value(row_all(mw, Max()), 0);
+        usum = lane_value(row_all(sw * exp2_fast((mw - um) * (inv_tau * kLog2e)), Add()), 0);
+      }
       const Factors f(a, own.w, usum != 0.0f, own.label >= 0, q, r);
-      if (more) next.template load<THREADS>(a, row1);
       if (f.zero) {
         blank(row);
         break;
       }
 
-      float term = 0.0f, p[EPT];
+      float term = 0.0f;
       const float lq = logf(q), lu = logf(usum);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) {
-        p[e] = own.id[e] >= 0 ? ue[e] / usum : 0.0f;
-        if (own.id[e] >= 0) term += entry_term(p[e], (own.u[e] - um) * inv_tau - lu, lq, se[e] - m, inv_tau);
+        ue[e] = exp2_fast((own.u[e] - um) * (inv_tau * kLog2e));
+        const float p = own.id[e] >= 0 ? ue[e] / usum : 0.0f;
+        if (own.id[e] >= 0) term += entry_term(p, (own.u[e] - um) * inv_tau - lu, lq, se[e] - m, inv_tau);
         if (e * THREADS + tid < a.K) {
           id_of[e * THREADS + tid] = own.id[e];
-          p_of[e * THREADS + tid] = p[e];
+          p_of[e * THREADS + tid] = p;
         }
       }
-      put<WAVES>(term, red[5], Add());
-      run = a.grad && more && next.w != 0.0f;
-      if (a.grad) {
+      term = wave_all(term, Add());
+      if (tid % 64 == 0) red[set][5][tid / 64] = term;
+      run = LOOP && more && next.w != 0.0f;
+      if (GRAD) {
         T* grad = grad_of(row);
         const T* s1 = logits_of(run ? row1 : row);
         const uint32_t limit = run ? last : 0;            // (else every thread loads the first pack once more)
+        Running<TWO> st1;
         asm volatile("" : "+v"(mine));
 #pragma unroll
-        for (int j = 0; j < NP; ++j) {
-          x[j].again();
-          if (there(j)) {
-            Pack<T, VEC> g;
+        for (int j = 0; j < NP + (LOOP ? kLag : 0); ++j) {
+          if (j < NP) {
+            x[j].again();
+            if (there(j)) {
+              P g;
 #pragma unroll
-            for (int c = 0; c < VEC; ++c) g.set(c, gradient_at<T, TWO>(x[j].get(c) - m, k, f));
-            g.store_stream(reinterpret_cast<T*>(reinterpret_cast<char*>(grad) + at(j)));
+              for (int c = 0; c < VEC; ++c) g.set(c, gradient_at<T, TWO>(x[j].get(c) - m, k, f));
+              g.store_stream(reinterpret_cast<T*>(reinterpret_cast<char*>(grad) + at(j)));
+            }
+            if (LOOP && bytes) x[j] = pack_of(j, s1, limit);
+            __builtin_amdgcn_sched_barrier(0);
           }
-          if (bytes) x[j] = pack_of(j, s1, limit);
-          __builtin_amdgcn_sched_barrier(0);
+          if (LOOP && j >= kLag) {
+            x[j - kLag].again();
+            st1.template add<P, VEC>(x[j - kLag], there(j - kLag), k);
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
+        st = st1;
         if (tid < tail) {
           grad[packed + tid] = from_float<T>(gradient_at<T, TWO>(xt - m, k, f));
-          xt = to_float(s1[packed + tid]);
+          if (LOOP) xt = to_float(s1[packed + tid]);
         }
       }
       __syncthreads();
       if (a.loss && tid == 0) {
-        float loss = 0.0f;
-        if (f.cs != 0.0f) loss += f.cs * a.tau * a.tau * take<WAVES>(red[5], Add());
+        float sum = 0.0f, loss = 0.0f;
+        for (int w = 0; w < WAVES; ++w) sum += red[set][5][w];
+        if (f.cs != 0.0f) loss += f.cs * a.tau * a.tau * sum;
         if (f.ch != 0.0f) loss += f.ch * (logf(r) - (sl - m));
         a.loss[row] = loss;
       }
       // the places of the entries and of the label once more, whole: an id that comes twice takes both shares
-      if (a.grad) {
+      if (GRAD) {
         T* grad = grad_of(row);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
@@ -322,7 +380,8 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
           if (!done) grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
         }
       }
-      __syncthreads();                         // red and the entries' arrays are written again
+      // (the entries' arrays are written again behind the next row's first barrier, which every reader of them has to reach)
+      set ^= 1;
       if (run) row = row1;
     }
     __syncthreads();
@@ -331,7 +390,9 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
 }
 
 // ---- rows that stream through ----
-// Longer rows than registers hold: a workgroup reads the row twice, the second time mostly from the last-level cache.  Few rows:
+// Longer rows than registers hold: a workgroup reads the row twice, the second time mostly from the last-level cache.  The loss alone
+// needs a row once and no registers to keep it in: more workgroups, more loads in flight (975 rows of 50021 fp16 28.4 us,
+// from a register tile 32.8).  Few rows:
 // `parts` workgroups take a row's columns; one launch leaves each part's maximum and sums in the workspace (and the logits at the
 // entries' places, which the gradient may overwrite), a second one joins them and does the rest.
 enum StreamMode : int { STREAM_ALL = 0, STREAM_STATS = 1, STREAM_REST = 2 };
@@ -347,7 +408,8 @@ constexpr int kStreamThreads = 512;
 template <typename T, bool TWO>
 __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamArgs t) {
   constexpr int VEC = kVec<T>, THREADS = kStreamThreads, WAVES = THREADS / 64, AHEAD = 4;
-  __shared__ float red[6][WAVES], p_of[kTopMax];
+  using P = Pack<T, VEC>;
+  __shared__ float red[6][16], p_of[kTopMax];
   __shared__ int32_t id_of[kTopMax];
   const DistillArgs& a = t.a;
   const int tid = threadIdx.x;
@@ -375,90 +437,49 @@ __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamAr
       }
       continue;
     }
-    float m = -kInf, q = 0.0f, r = 0.0f;
+    Running<TWO> st;
     if (t.mode != STREAM_REST) {
-      // running maximum and sums of this thread's columns
-      auto more = [&](float best, auto&& each) {
-        const float m1 = fmaxf(m, best), base = m1 == -kInf ? 0.0f : m1;
-        q *= exp2_fast((m - base) * k.kq);
-        if (TWO) r *= exp2_fast((m - base) * k.kr);
-        each(base);
-        m = m1;
-      };
       for (int32_t c = c0 + tid * VEC; c < packed; c += THREADS * VEC * AHEAD) {
-        Pack<T, VEC> x[AHEAD];
+        P x[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) x[j] = Pack<T, VEC>::load(s + min(c + j * THREADS * VEC, packed - VEC));
+        for (int j = 0; j < AHEAD; ++j) x[j] = P::load(s + min(c + j * THREADS * VEC, packed - VEC));
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-          if (c + j * THREADS * VEC >= packed) break;
-          float best = x[j].get(0);
-#pragma unroll
-          for (int e = 1; e < VEC; ++e) best = fmaxf(best, x[j].get(e));
-          more(best, [&](float base) {
-            float qs = 0.0f, rs = 0.0f;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-              const float y = x[j].get(e) - base;
-              qs += exp2_fast(y * k.kq);
-              if (TWO) rs += exp2_fast(y * k.kr);
-            }
-            q += qs;
-            r += rs;
-          });
-        }
+        for (int j = 0; j < AHEAD; ++j) st.template add<P, VEC>(x[j], c + j * THREADS * VEC < packed, k);
       }
-      if (packed + tid < c1) {
-        const float y0 = to_float(s[packed + tid]);
-        more(y0, [&](float base) {
-          q += exp2_fast((y0 - base) * k.kq);
-          if (TWO) r += exp2_fast((y0 - base) * k.kr);
-        });
-      }
-      const float mine = m;
-      put<WAVES>(m, red[0], Max());
-      __syncthreads();
-      m = take<WAVES>(red[0], Max());
-      const float base = m == -kInf ? 0.0f : m;
-      q *= exp2_fast((mine - base) * k.kq);
-      if (TWO) r *= exp2_fast((mine - base) * k.kr);
-      put<WAVES>(q, red[2], Add());
-      if (TWO) put<WAVES>(r, red[3], Add());
-      __syncthreads();
-      q = take<WAVES>(red[2], Add());
-      r = TWO ? take<WAVES>(red[3], Add()) : q;
-      if (t.mode == STREAM_STATS) {
-        if (tid == 0) {
-          float* st = t.stats + unit * 4;
-          st[0] = m;
-          st[1] = q;
-          st[2] = r;
-        }
-        // the logits that this part has for the entries and the label
-        float* values = t.values + row * (a.K + 1);
-        if (own.id[0] >= c0 && own.id[0] < c1) values[tid] = to_float(s[own.id[0]]);
-        if (tid == 0 && own.label >= c0 && own.label < c1) values[a.K] = to_float(s[own.label]);
-        continue;
-      }
+      if (packed + tid < c1) st.add(to_float(s[packed + tid]), k);
     } else {
-      // join the parts: the same order in every workgroup
-      const float* st = t.stats + row * t.parts * 4;
-      for (int32_t j = tid; j < t.parts; j += THREADS) m = fmaxf(m, st[j * 4]);
-      put<WAVES>(m, red[0], Max());
-      __syncthreads();
-      m = take<WAVES>(red[0], Max());
-      const float base = m == -kInf ? 0.0f : m;
+      // the parts' statistics: the same order in every workgroup
+      const float* parts = t.stats + row * t.parts * 4;
       for (int32_t j = tid; j < t.parts; j += THREADS) {
-        q += st[j * 4 + 1] * exp2_fast((st[j * 4] - base) * k.kq);
-        r += st[j * 4 + 2] * exp2_fast((st[j * 4] - base) * (TWO ? k.kr : k.kq));
+        Running<TWO> one;
+        one.m = parts[j * 4];
+        one.q = parts[j * 4 + 1];
+        one.r = parts[j * 4 + 2];
+        const float m1 = fmaxf(st.m, one.m);
+        one.rise(m1, k);
+        st.rise(m1, k);
+        st.q += one.q;
+        if (TWO) st.r += one.r;
       }
-      put<WAVES>(q, red[2], Add());
-      put<WAVES>(r, red[3], Add());
-      __syncthreads();
-      q = take<WAVES>(red[2], Add());
-      r = take<WAVES>(red[3], Add());
     }
-    if (m == -kInf) m = 0.0f;
+    st.over_wave(k);
+    st.put(red);
+    __syncthreads();
+    st.template take<WAVES>(red, k);
+    if (t.mode == STREAM_STATS) {
+      if (tid == 0) {
+        float* out = t.stats + unit * 4;
+        out[0] = st.m;
+        out[1] = st.q;
+        out[2] = st.r;
+      }
+      // the logits that this part has for the entries and the label
+      float* values = t.values + row * (a.K + 1);
+      if (own.id[0] >= c0 && own.id[0] < c1) values[tid] = to_float(s[own.id[0]]);
+      if (tid == 0 && own.label >= c0 && own.label < c1) values[a.K] = to_float(s[own.label]);
+      continue;
+    }
+    const float m = in_vgpr(st.m), q = st.q, r = st.r;
     float se = 0.0f, sl = 0.0f;
     if (t.mode == STREAM_REST) {
       const float* values = t.values + row * (a.K + 1);
@@ -469,15 +490,17 @@ __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamAr
       if (own.label >= 0) sl = to_float(s[own.label]);
       asm volatile("" ::"v"(se), "v"(sl));
     }
-    float um = own.u[0];
-    put<WAVES>(um, red[1], Max());
+    float um = wave_all(fmaxf(own.u[0], kLowest), Max());
+    if (tid % 64 == 0) red[3][tid / 64] = um;
     __syncthreads();
-    um = take<WAVES>(red[1], Max());
-    if (um == -kInf) um = 0.0f;
-    const float ue = exp2_fast((own.u[0] - um) * inv_tau * kLog2e);
-    put<WAVES>(ue, red[4], Add());
+    um = red[3][0];
+    for (int w = 1; w < WAVES; ++w) um = fmaxf(um, red[3][w]);
+    const float ue = exp2_fast((own.u[0] - um) * (inv_tau * kLog2e));
+    float usum = wave_all(ue, Add());
+    if (tid % 64 == 0) red[4][tid / 64] = usum;
     __syncthreads();
-    const float usum = take<WAVES>(red[4], Add());
+    usum = 0.0f;
+    for (int w = 0; w < WAVES; ++w) usum += red[4][w];
     const Factors f(a, own.w, usum != 0.0f, own.label >= 0, q, r);
     const float p = own.id[0] >= 0 ? ue / usum : 0.0f;
     float term = 0.0f;
@@ -486,7 +509,8 @@ __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamAr
       id_of[tid] = own.id[0];
       p_of[tid] = p;
     }
-    put<WAVES>(term, red[5], Add());
+    term = wave_all(term, Add());
+    if (tid % 64 == 0) red[5][tid / 64] = term;
     if (grad) {
       for (int32_t c = c0 + tid * VEC; c < packed; c += THREADS * VEC * AHEAD) {
         Pack<T, VEC> x[AHEAD];
@@ -506,7 +530,9 @@ __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamAr
     __syncthreads();
     if (a.loss && tid == 0 && part == 0) {
       float loss = 0.0f;
-      if (f.cs != 0.0f) loss += f.cs * a.tau * a.tau * take<WAVES>(red[5], Add());
+      float sum = 0.0f;
+      for (int w = 0; w < WAVES; ++w) sum += red[5][w];
+      if (f.cs != 0.0f) loss += f.cs * a.tau * a.tau * sum;
       if (f.ch != 0.0f) loss += f.ch * (logf(r) - (sl - m));
       a.loss[row] = loss;
     }
@@ -528,12 +554,13 @@ __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamAr
 
 constexpr int64_t kMostRowBlocks = 1 << 21;       // (a launch has fewer than 2^32 threads)
 
-template <typename T, bool TWO> hipError_t launch(const DistillArgs& a, hipStream_t st) {
+template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.n * a.T;
   const DistillPlan plan = plan_distill(rows, a.V, a.K, a.type);
   const int32_t packs = a.V / kVec<T>;
   const uint32_t blocks = (uint32_t)std::min(rows, kMostRowBlocks);
-  if (plan.parts > 1 || packs > 1024 * 16) {
+  // (the loss alone, of rows of more than 256 packs)
+  if (plan.parts > 1 || packs > 1024 * 16 || (!GRAD && packs > 256)) {
     StreamArgs t{a, rows, plan.parts, plan.cols, STREAM_ALL, nullptr, nullptr};
     const dim3 grid((uint32_t)std::min(rows * plan.parts, kMostRowBlocks)), block(kStreamThreads);
     if (plan.parts > 1) {
@@ -546,14 +573,25 @@ template <typename T, bool TWO> hipError_t launch(const DistillArgs& a, hipStrea
     distill_stream_kernel<T, TWO><<<grid, block, 0, st>>>(t);
     return hipGetLastError();
   }
-  if (packs <= 64) distill_row_kernel<T, 64, 1, TWO><<<dim3(blocks), dim3(64), 0, st>>>(a, rows);
-  else if (packs <= 64 * 4) distill_row_kernel<T, 64, 4, TWO><<<dim3(blocks), dim3(64), 0, st>>>(a, rows);
-  else if (packs <= 256 * 4) distill_row_kernel<T, 256, 4, TWO><<<dim3(blocks), dim3(256), 0, st>>>(a, rows);
-  else if (packs <= 256 * 8) distill_row_kernel<T, 256, 8, TWO><<<dim3(blocks), dim3(256), 0, st>>>(a, rows);
-  else if (packs <= 256 * 16) distill_row_kernel<T, 256, 16, TWO><<<dim3(blocks), dim3(256), 0, st>>>(a, rows);
-  else if (packs <= 512 * 16) distill_row_kernel<T, 512, 16, TWO><<<dim3(blocks), dim3(512), 0, st>>>(a, rows);
-  else distill_row_kernel<T, 1024, 16, TWO><<<dim3((uint32_t)std::min<int64_t>(rows, 256)), dim3(1024), 0, st>>>(a, rows);
+  // As many threads as the row needs with 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
+  // unit, of which some load while others compute: one row each (7936 rows of 32000 bf16, two softmaxes 206 us; looping, with the
+  // next row's loads in between, 242).  Rows of 1024 threads have the compute unit to themselves and loop (15872 rows of
+  // 128000 bf16 1605 us; loads between the rows 1840).
+  if (packs <= 64) distill_row_kernel<T, 64, 1, TWO, GRAD, false><<<blocks, dim3(64), 0, st>>>(a, rows);
+  else if (packs <= 64 * 4) distill_row_kernel<T, 64, 4, TWO, GRAD, false><<<blocks, dim3(64), 0, st>>>(a, rows);
+  else if constexpr (GRAD) {
+    if (packs <= 256 * 4) distill_row_kernel<T, 256, 4, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
+    else if (packs <= 256 * 8) distill_row_kernel<T, 256, 8, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
+    else if (packs <= 256 * 16) distill_row_kernel<T, 256, 16, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
+    else if (packs <= 512 * 16) distill_row_kernel<T, 512, 16, TWO, true, false><<<blocks, dim3(512), 0, st>>>(a, rows);
+    else distill_row_kernel<T, 1024, 16, TWO, true, true><<<dim3((uint32_t)std::min<int64_t>(rows, 256)), dim3(1024), 0, st>>>(a, rows);
+  }
   return hipGetLastError();
+}
+
+template <typename T> hipError_t by_terms(const DistillArgs& a, bool two, hipStream_t st) {
+  if (two) return a.grad ? launch<T, true, true>(a, st) : launch<T, true, false>(a, st);
+  return a.grad ? launch<T, false, true>(a, st) : launch<T, false, false>(a, st);
 }
 
 }  // namespace
@@ -581,9 +619,8 @@ DistillPlan plan_distill(int64_t rows, int32_t V, int32_t K, int type) {
 hipError_t launch_distill(const DistillArgs& a, hipStream_t st) {
   // both terms at a temperature other than 1: two softmaxes
   const bool two = a.K > 0 && a.hard > 0.0f && a.hard < 1.0f && a.tau != 1.0f;
-  if (a.type == TYPE_F32) return two ? launch<float, true>(a, st) : launch<float, false>(a, st);
-  if (a.type == TYPE_BF16) return two ? launch<bf16_t, true>(a, st) : launch<bf16_t, false>(a, st);
-  return two ? launch<_Float16, true>(a, st) : launch<_Float16, false>(a, st);
+  if (a.type == TYPE_F32) return by_terms<float>(a, two, st);
+  return a.type == TYPE_BF16 ? by_terms<bf16_t>(a, two, st) : by_terms<_Float16>(a, two, st);
 }
 
 }  // namespace ceca

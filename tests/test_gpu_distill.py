@@ -88,10 +88,14 @@ def _check(env, dtype, logits, top, ids, labels, weight, peer, temperature, hard
         assert ((np.isnan(g) & np.isnan(want_grad)) | (np.abs(g - want_grad) <= bound)).all()
     if extra or offset:
         assert (gflat[:offset] == 9).all() and (gflat[offset:].view(n * T, V + extra)[:, V:] == 9).all()
-    # one output alone, and the gradient over the logits, give the same bits
-    loss2 = torch.empty_like(loss)
+    # the loss alone (which may add up in another order) keeps to the same bound; the gradient alone, and over the logits, has the same
+    # bits
+    loss2 = torch.full_like(loss, float("nan"))
     P.ceca_distill(spec, loss=loss2, workspace=ws)
-    assert torch.equal(loss.view(torch.int32), loss2.view(torch.int32))
+    alone = loss2.double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        same = (alone == want_loss) | (np.isnan(alone) & np.isnan(want_loss))
+        assert (same | (np.abs(alone - want_loss) <= delta * size)).all()
     whole = torch.int32 if dtype == "float32" else torch.int16
     bits = grad.contiguous().view(whole)
     grad2 = torch.empty_like(grad).fill_(9.0)
