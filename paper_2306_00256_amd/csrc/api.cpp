@@ -1480,7 +1480,7 @@ int32_t ceca_distill(const ceca_distill_t* spec, float* loss, void* grad, int64_
 int64_t ceca_top_logits_workspace_bytes(int32_t type, int32_t rows, int32_t V, int32_t K) {
   const int32_t rc = check_top(type, rows, V, K);
   if (rc != CECA_OK) return rc;
-  return 0;
+  return ceca::plan_top(rows, V, K, type).bytes;
 }
 
 int32_t ceca_top_logits(const void* logits, int32_t type, int64_t ld, int32_t rows, int32_t V, int32_t K, float* top, int32_t* ids,
@@ -1496,11 +1496,13 @@ int32_t ceca_top_logits(const void* logits, int32_t type, int64_t ld, int32_t ro
   if (!span_bytes(rows, ld, V, size, &sb)) return fail(CECA_EINVAL, "sizes beyond the address space");
   if (overlaps(logits, sb, top, out) || overlaps(logits, sb, ids, out) || overlaps(top, out, ids, out))
     return fail(CECA_EINVAL, "an output overlaps the logits or the other output");
+  if (need > 0 && (overlaps(workspace, need, logits, sb) || overlaps(workspace, need, top, out) || overlaps(workspace, need, ids, out)))
+    return fail(CECA_EINVAL, "the workspace overlaps an argument");
   const int32_t rc = check_workspace(workspace, workspace_bytes, need);
   if (rc != CECA_OK) return rc;
   ceca::TopArgs a{};
   a.logits = logits;  a.ld = ld;  a.top = top;  a.ids = ids;
-  a.rows = rows;  a.V = V;  a.K = K;  a.type = type;
+  a.rows = rows;  a.V = V;  a.K = K;  a.type = type;  a.workspace = workspace;
   const hipError_t e = ceca::launch_top(a, (hipStream_t)hip_stream);
   return e == hipSuccess ? CECA_OK : hip_fail(e, "top logits kernel launch");
 }

@@ -16,30 +16,8 @@ namespace ceca {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kInf = __builtin_inff();
-
-// Over a wavefront's rows of 16 lanes in four steps without LDS, then over the four rows: the same for every lane.
-template <int CTRL> __device__ __forceinline__ float dpp(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-template <typename F> __device__ __forceinline__ float row_all(float v, F f) {
-  v = f(v, dpp<0xB1>(v));        // lanes 1 apart
-  v = f(v, dpp<0x4E>(v));        // 2
-  v = f(v, dpp<0x141>(v));       // the other four of eight
-  return f(v, dpp<0x140>(v));    // the other eight of sixteen
-}
-__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
-template <typename F> __device__ __forceinline__ float wave_all(float v, F f) {
-  v = row_all(v, f);
-  return f(f(lane_value(v, 0), lane_value(v, 16)), f(lane_value(v, 32), lane_value(v, 48)));
-}
-struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
-struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };     // drops NaN
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }       // zero below 2^-126
-
-// Columns a thread reads at once: 16 bytes.
-template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
 
 // What is known of a row before its logits are: every thread has its entries (EPT of them).
 template <int EPT> struct Entries {

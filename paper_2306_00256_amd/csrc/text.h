@@ -93,7 +93,17 @@ struct TopArgs {
   int32_t* ids;
   int32_t rows, V, K;
   int32_t type;
+  void* workspace;         // of plan_top(...).bytes
 };
+
+// Rows go through `parts` workgroups of `cols` columns (the last one may have fewer); with several, each leaves its K largest in the
+// workspace, and further launches make one list of up to kMergeWords / K at a time, back and forth between two parts of it.
+constexpr int kMergeWords = 4096;
+struct TopPlan {
+  int32_t parts, cols;
+  int64_t second, bytes;   // offset of the workspace's second part
+};
+TopPlan plan_top(int64_t rows, int32_t V, int32_t K, int type);
 
 constexpr int kTopMax = 256;         // most entries of a row's top logits
 

@@ -50,4 +50,27 @@ template <typename T, int VEC> struct Pack {
   __device__ __forceinline__ void set(int k, float x) { v[k] = __builtin_bit_cast(R, from_float<T>(x)); }
 };
 
+constexpr float kInf = __builtin_inff();
+
+// Over a wavefront's rows of 16 lanes in four steps without LDS, then over the four rows: the same for every lane.
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <typename F> __device__ __forceinline__ float row_all(float v, F f) {
+  v = f(v, dpp<0xB1>(v));        // lanes 1 apart
+  v = f(v, dpp<0x4E>(v));        // 2
+  v = f(v, dpp<0x141>(v));       // the other four of eight
+  return f(v, dpp<0x140>(v));    // the other eight of sixteen
+}
+__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+template <typename F> __device__ __forceinline__ float wave_all(float v, F f) {
+  v = row_all(v, f);
+  return f(f(lane_value(v, 0), lane_value(v, 16)), f(lane_value(v, 32), lane_value(v, 48)));
+}
+struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };     // drops NaN
+
+// Columns a thread reads at once: 16 bytes.
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
+
 }  // namespace ceca

@@ -1,4 +1,13 @@
 // The largest logits of a row and their places.
+//
+// What bounds it: the row is read once.  A workgroup holds a row (or a part of it) in registers and looks for a threshold that at least
+// K logits reach and few more: the K-th largest of the maxima of its threads' shares does, since every share that reaches it has
+// such a logit.  What reaches the threshold goes to LDS, where a candidate's rank is the number of candidates before it.
+// Where too many do (equal logits, few shares), the K-th largest logit itself is found bit by bit, and among its equals the
+// last place that still belongs.  Candidates are ordered by one word of (value, place): the same result whatever the order in which
+// they were put into LDS.
+#include <algorithm>
+
 #include "device_util.h"
 #include "text_util.h"
 
@@ -6,54 +15,329 @@ namespace ceca {
 
 namespace {
 
-// Order of the logits as unsigned numbers: -inf < ... < -0 = +0 < ... < +inf < NaN.
-__device__ __forceinline__ uint32_t order_key(float v) {
-  if (v != v) return 0xffc00000u;
-  const uint32_t b = __float_as_uint(v + 0.0f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+// Order of the logits as whole numbers of kBits<T> bits: -inf < ... < -0 = +0 < ... < +inf < NaN.
+template <typename T> constexpr int kBits = 8 * (int)sizeof(T);
+template <typename T> struct Order;
+template <> struct Order<float> {
+  static constexpr uint32_t sign = 0x80000000u, all = 0xffffffffu, inf = 0x7f800000u;
+  __device__ static __forceinline__ uint32_t raw(float x) { return __float_as_uint(x); }
+  __device__ static __forceinline__ float value(uint32_t b) { return __uint_as_float(b); }
+};
+template <> struct Order<bf16_t> {
+  static constexpr uint32_t sign = 0x8000u, all = 0xffffu, inf = 0x7f80u;
+  __device__ static __forceinline__ uint32_t raw(float x) { return __float_as_uint(x) >> 16; }        // (x came from one: exact)
+  __device__ static __forceinline__ float value(uint32_t b) { return __uint_as_float(b << 16); }
+};
+template <> struct Order<_Float16> {
+  static constexpr uint32_t sign = 0x8000u, all = 0xffffu, inf = 0x7c00u;
+  __device__ static __forceinline__ uint32_t raw(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+  __device__ static __forceinline__ float value(uint32_t b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)b); }
+};
+template <typename T> __device__ __forceinline__ uint32_t key_of(float x) {
+  using O = Order<T>;
+  uint32_t b = O::raw(x + 0.0f);                              // -0 becomes +0
+  if (x != x) b = O::inf | 1;                                 // one NaN for all
+  return b & O::sign ? ~b & O::all : b | O::sign;
 }
-constexpr uint32_t kKeyMinusInf = 0x007fffffu;
+template <typename T> __device__ __forceinline__ float value_of(uint32_t key) {
+  using O = Order<T>;
+  return O::value(key & O::sign ? key ^ O::sign : ~key & O::all);
+}
+template <typename T> constexpr uint32_t kLeastKey = (~(Order<T>::inf | Order<T>::sign) & Order<T>::all) + 1;    // above -inf
 
-// One workgroup per row picks the largest of what is left, K times.
-template <typename T>
-__global__ __launch_bounds__(256) void top_kernel(TopArgs a) {
-  __shared__ uint64_t best[4];
-  const int64_t row = blockIdx.x;
-  const T* s = static_cast<const T*>(a.logits) + row * a.ld;
-  uint64_t last = ~0ull;
-  for (int k = 0; k < a.K; ++k) {
-    uint64_t b = 0;
-    for (int32_t v = threadIdx.x; v < a.V; v += 256) {
-      const uint64_t key = (uint64_t)order_key(to_float(s[v])) << 32 | (uint32_t)~v;
-      if (key < last && key > b) b = key;
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t c = __shfl_xor((unsigned long long)b, o, 64);
-      b = c > b ? c : b;
-    }
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) best[threadIdx.x / 64] = b;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) b = best[w] > b ? best[w] : b;
-    last = b;
-    if (threadIdx.x == 0) {
-      const bool is = (uint32_t)(b >> 32) > kKeyMinusInf;
-      const int32_t at = (int32_t)~(uint32_t)b;
-      a.top[row * a.K + k] = is ? to_float(s[at]) : -__builtin_inff();
-      a.ids[row * a.K + k] = is ? at : -1;
+constexpr int kMostCandidates = 1024;
+
+// Candidates in LDS to their ranks: the K first go out, as values and places or, from a part of a row, as they are.
+template <typename T, int THREADS>
+__device__ __forceinline__ void rank_and_store(const uint64_t* cand, int count, int K, float* top, int32_t* ids, uint64_t* words) {
+  for (int c = threadIdx.x; c < max(count, K); c += THREADS) {
+    if (c < count) {
+      const uint64_t own = cand[c];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < count; ++j) rank += cand[j] > own;
+      if (rank < K) {
+        if (words) {
+          words[rank] = own;
+        } else {
+          top[rank] = value_of<T>((uint32_t)(own >> 32));
+          ids[rank] = (int32_t)~(uint32_t)own;
+        }
+      }
+    } else {                                                  // fewer than K that are not masked
+      if (words) {
+        words[c] = 0;
+      } else {
+        top[c] = -kInf;
+        ids[c] = -1;
+      }
     }
   }
 }
 
+// Whole numbers over the workgroup (below 2^24: fp32 sums are exact).
+template <int THREADS> __device__ __forceinline__ int count_all(int mine, float* slot) {
+  const float w = wave_all((float)mine, Add());
+  if (THREADS == 64) return (int)w;
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) slot[threadIdx.x / 64] = w;
+  __syncthreads();
+  float sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < THREADS / 64; ++k) sum += slot[k];
+  return (int)sum;
+}
+
+template <typename T, int THREADS, int NP>
+__global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs a, TopPlan plan) {
+  constexpr int VEC = kVec<T>, WAVES = THREADS / 64;
+  using P = Pack<T, VEC>;
+  __shared__ uint64_t cand[kMostCandidates];
+  __shared__ uint32_t group[2 * THREADS], threshold;
+  __shared__ float slot[WAVES];
+  __shared__ int found;
+  const int tid = threadIdx.x;
+  for (int64_t unit = blockIdx.x; unit < (int64_t)a.rows * plan.parts; unit += gridDim.x) {
+    const int64_t row = unit / plan.parts;
+    const int32_t c0 = (int32_t)(unit - row * plan.parts) * plan.cols, cols = min(plan.cols, a.V - c0);
+    const T* s = static_cast<const T*>(a.logits) + row * a.ld + c0;
+    // packs as in the distillation's register tiles: by their distance from the beginning, the last one in place of those past it
+    const int32_t packed = cols / VEC * VEC, tail = cols - packed;
+    const uint32_t bytes = (uint32_t)packed * sizeof(T), last = bytes ? bytes - 16 : 0;
+    uint32_t mine = tid * 16;
+    auto at = [&](int j) { return mine + (uint32_t)(j * THREADS * 16); };
+    auto there = [&](int j) { return at(j) < bytes; };
+    P x[NP];
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      if (bytes) {
+        x[j] = P::load_stream(reinterpret_cast<const T*>(reinterpret_cast<const char*>(s) + min(at(j), last)));
+      } else {
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) x[j].set(c, -kInf);
+      }
+    }
+    float xt = tid < tail ? to_float(s[packed + tid]) : -kInf;
+    __syncthreads();                                           // (LDS of the unit before)
+    if (tid == 0) found = 0;
+
+    // f(value, place in the row, whether it is one) for every logit of this thread
+    auto each = [&](auto&& f) {
+      asm volatile("" : "+v"(mine));
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        x[j].again();
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) f(x[j].get(c), c0 + (int32_t)(at(j) / sizeof(T)) + c, there(j));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      f(xt, c0 + packed + tid, tid < tail);
+    };
+    auto put = [&](float v, int32_t place) {
+      const int k = atomicAdd(&found, 1);
+      if (k < kMostCandidates) cand[k] = (uint64_t)key_of<T>(v) << 32 | (uint32_t)~place;
+    };
+
+    bool exact = THREADS == 64;
+    if (!exact) {
+      // two shares per thread; a pack past the last one must not count twice
+      float g0 = xt, g1 = -kInf;
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        float best = x[j].get(0);
+#pragma unroll
+        for (int c = 1; c < VEC; ++c) best = fmaxf(best, x[j].get(c));
+        best = there(j) ? best : -kInf;
+        if (j % 2) g1 = fmaxf(g1, best);
+        else g0 = fmaxf(g0, best);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      group[tid] = key_of<T>(g0);
+      group[THREADS + tid] = key_of<T>(g1);
+      __syncthreads();
+      if (tid < 64) {
+        // the K-th largest share's maximum, from above, to 20 bits (what the others may add are few candidates more)
+        constexpr int EACH = 2 * THREADS / 64;
+        uint32_t key[EACH], t = 0;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) key[e] = group[e * 64 + tid];
+        for (int bit = kBits<T> - 1; bit >= std::max(kBits<T> - 20, 0); --bit) {
+          const uint32_t t1 = t | 1u << bit;
+          int n = 0;
+#pragma unroll
+          for (int e = 0; e < EACH; ++e) n += __builtin_popcountll(__ballot(key[e] >= t1));
+          if (n >= a.K) t = t1;
+          if (n == a.K) break;
+        }
+        if (tid == 0) threshold = max(t, kLeastKey<T>);
+      }
+      __syncthreads();
+      const float least = value_of<T>(threshold);
+      asm volatile("" : "+v"(mine));
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        x[j].again();
+        bool some = false;
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) some |= !(x[j].get(c) < least);           // (NaN too)
+        if (there(j) && some) {
+          x[j].again();
+#pragma unroll
+          for (int c = 0; c < VEC; ++c)
+            if (!(x[j].get(c) < least)) put(x[j].get(c), c0 + (int32_t)(at(j) / sizeof(T)) + c);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (tid < tail && !(xt < least)) put(xt, c0 + packed + tid);
+      __syncthreads();
+      exact = found > kMostCandidates;
+    }
+    if (exact) {
+      // the K-th largest key, bit by bit; masked logits are none
+      auto count = [&](auto&& is) {
+        int n = 0;
+        each([&](float v, int32_t place, bool one) {
+          const uint32_t key = key_of<T>(v);
+          n += one && key >= kLeastKey<T> && is(key, place) ? 1 : 0;
+        });
+        return count_all<THREADS>(n, slot);
+      };
+      uint32_t t = 0;
+      for (int bit = kBits<T> - 1; bit >= 0; --bit) {
+        const uint32_t t1 = t | 1u << bit;
+        if (count([&](uint32_t key, int32_t) { return key >= t1; }) >= a.K) t = t1;
+      }
+      // how many of its equals belong, and the place of the last of them (t = 0: fewer than K logits, all belong)
+      const int need = a.K - count([&](uint32_t key, int32_t) { return key > t; });
+      int32_t end = 0;
+      if (t != 0) {
+        for (int bit = 30 - __builtin_clz((uint32_t)a.V | 1) + 1; bit >= 0; --bit) {
+          const int32_t end1 = end + (1 << bit);
+          if (count([&](uint32_t key, int32_t place) { return key == t && place < end1; }) < need) end = end1;
+        }
+      }
+      __syncthreads();
+      if (tid == 0) found = 0;
+      __syncthreads();
+      each([&](float v, int32_t place, bool one) {
+        const uint32_t key = key_of<T>(v);
+        if (one && key >= kLeastKey<T> && (key > t || (key == t && place <= end))) put(v, place);
+      });
+      __syncthreads();
+    }
+    float* top = a.top + row * a.K;
+    int32_t* ids = a.ids + row * a.K;
+    rank_and_store<T, THREADS>(cand, min(found, kMostCandidates), a.K, top, ids, plan.parts > 1 ? static_cast<uint64_t*>(a.workspace) + unit * a.K : nullptr);
+  }
+}
+
+// One list of K from up to `per` of a row's `lists` lists of K (each from the largest down, zeros behind).  At least K words reach the
+// largest of the lists' last ones; where too many do, the K-th largest is found bit by bit (all words but zeros differ).
+constexpr int kMergeThreads = 256, kMergeEach = kMergeWords / kMergeThreads;
+struct MergeArgs {
+  TopArgs a;
+  const uint64_t* in;
+  uint64_t* out;               // null: to top and ids
+  int32_t lists, per, groups;  // per row: lists, lists per workgroup, workgroups
+};
+template <typename T>
+__global__ __launch_bounds__(kMergeThreads) void top_merge_kernel(MergeArgs m) {
+  __shared__ uint64_t cand[kMostCandidates];
+  __shared__ unsigned long long least;
+  __shared__ float slot[kMergeThreads / 64];
+  __shared__ int found;
+  const int tid = threadIdx.x, K = m.a.K;
+  for (int64_t unit = blockIdx.x; unit < (int64_t)m.a.rows * m.groups; unit += gridDim.x) {
+    const int64_t row = unit / m.groups;
+    const int32_t first = (int32_t)(unit - row * m.groups) * m.per, lists = min(m.per, m.lists - first), all = lists * K;
+    const uint64_t* words = m.in + (row * m.lists + first) * K;
+    uint64_t w[kMergeEach];
+#pragma unroll
+    for (int e = 0; e < kMergeEach; ++e) w[e] = e * kMergeThreads + tid < all ? words[e * kMergeThreads + tid] : 0;
+    const uint64_t end = tid < lists ? words[tid * K + K - 1] : 0;
+    __syncthreads();
+    if (tid == 0) {
+      found = 0;
+      least = 1;
+    }
+    __syncthreads();
+    if (end > 1) atomicMax(&least, (unsigned long long)end);
+    __syncthreads();
+    uint64_t t = least;
+    auto collect = [&]() {
+#pragma unroll
+      for (int e = 0; e < kMergeEach; ++e)
+        if (w[e] >= t) {
+          const int k = atomicAdd(&found, 1);
+          if (k < kMostCandidates) cand[k] = w[e];
+        }
+      __syncthreads();
+    };
+    collect();
+    if (found > kMostCandidates) {
+      t = 0;
+      for (int bit = 31 + kBits<T>; bit >= 0; --bit) {
+        const uint64_t t1 = t | 1ull << bit;
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < kMergeEach; ++e) n += w[e] >= t1;
+        if (count_all<kMergeThreads>(n, slot) >= K) t = t1;
+      }
+      t = max(t, (uint64_t)1);
+      __syncthreads();
+      if (tid == 0) found = 0;
+      __syncthreads();
+      collect();
+    }
+    rank_and_store<T, kMergeThreads>(cand, min(found, kMostCandidates), K, m.a.top + row * K, m.a.ids + row * K, m.out ? m.out + unit * K : nullptr);
+  }
+}
+
+constexpr int64_t kMostTopBlocks = 1 << 22;
+
+template <typename T> hipError_t launch(const TopArgs& a, hipStream_t st) {
+  const TopPlan plan = plan_top(a.rows, a.V, a.K, a.type);
+  const int32_t packs = plan.cols / kVec<T>;
+  const dim3 grid((uint32_t)std::min((int64_t)a.rows * plan.parts, kMostTopBlocks));
+  if (packs <= 64) top_kernel<T, 64, 1><<<grid, dim3(64), 0, st>>>(a, plan);
+  else if (packs <= 64 * 4) top_kernel<T, 64, 4><<<grid, dim3(64), 0, st>>>(a, plan);
+  else if (packs <= 256 * 4) top_kernel<T, 256, 4><<<grid, dim3(256), 0, st>>>(a, plan);
+  else if (packs <= 256 * 8) top_kernel<T, 256, 8><<<grid, dim3(256), 0, st>>>(a, plan);
+  else top_kernel<T, 256, 16><<<grid, dim3(256), 0, st>>>(a, plan);
+  uint64_t *in = static_cast<uint64_t*>(a.workspace), *out = in + plan.second / 8;
+  for (int32_t lists = plan.parts; lists > 1;) {
+    MergeArgs m{a, in, out, lists, kMergeWords / a.K, 0};
+    m.groups = (lists + m.per - 1) / m.per;
+    if (m.groups == 1) m.out = nullptr;
+    top_merge_kernel<T><<<dim3((uint32_t)std::min((int64_t)a.rows * m.groups, kMostTopBlocks)), dim3(kMergeThreads), 0, st>>>(m);
+    lists = m.groups;
+    std::swap(in, out);
+  }
+  return hipGetLastError();
+}
+
 }  // namespace
 
+TopPlan plan_top(int64_t rows, int32_t V, int32_t K, int type) {
+  TopPlan p{};
+  const int32_t vec = type == TYPE_F32 ? 4 : 8, most = 256 * 16 * vec;     // columns of the largest register tile
+  // parts that registers hold; few rows in parts of 4096 columns or more, up to 1024 workgroups and one merge
+  int64_t parts = (V + (int64_t)most - 1) / most;
+  if (rows > 0) parts = std::max(parts, std::min<int64_t>({V / 4096, 1024 / rows, kMergeWords / K}));
+  parts = std::max<int64_t>(parts, 1);
+  p.cols = (int32_t)(((V + parts - 1) / parts + vec - 1) / vec * vec);
+  p.parts = (V + p.cols - 1) / p.cols;
+  if (p.parts > 1) {
+    const int64_t groups = (p.parts + kMergeWords / K - 1) / (kMergeWords / K);
+    p.second = (rows * p.parts * K * 8 + 255) / 256 * 256;
+    p.bytes = p.second + (groups > 1 ? (rows * groups * K * 8 + 255) / 256 * 256 : 0);
+  }
+  return p;
+}
+
 hipError_t launch_top(const TopArgs& a, hipStream_t st) {
-  const dim3 grid((uint32_t)a.rows), block(256);
-  if (a.type == TYPE_F32) top_kernel<float><<<grid, block, 0, st>>>(a);
-  else if (a.type == TYPE_BF16) top_kernel<bf16_t><<<grid, block, 0, st>>>(a);
-  else top_kernel<_Float16><<<grid, block, 0, st>>>(a);
-  return hipGetLastError();
+  if (a.type == TYPE_F32) return launch<float>(a, st);
+  return a.type == TYPE_BF16 ? launch<bf16_t>(a, st) : launch<_Float16>(a, st);
 }
 
 }  // namespace ceca
