@@ -121,17 +121,24 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
     __syncthreads();                                           // (LDS of the unit before)
     if (tid == 0) found = 0;
 
-    // f(value, place in the row, whether it is one) for every logit of this thread
+    // f(value, place) for every logit of this thread: from the registers of a small tile, else, for the few rows that take the long
+    // way, from memory once more (kept for that, a large tile's logits would cost every row registers)
     auto each = [&](auto&& f) {
-      asm volatile("" : "+v"(mine));
+      if constexpr (THREADS == 64) {
 #pragma unroll
-      for (int j = 0; j < NP; ++j) {
-        x[j].again();
+        for (int j = 0; j < NP; ++j)
+          if (there(j)) {
 #pragma unroll
-        for (int c = 0; c < VEC; ++c) f(x[j].get(c), c0 + (int32_t)(at(j) / sizeof(T)) + c, there(j));
-        __builtin_amdgcn_sched_barrier(0);
+            for (int c = 0; c < VEC; ++c) f(x[j].get(c), c0 + (int32_t)(at(j) / sizeof(T)) + c);
+          }
+      } else {
+        for (int32_t c = tid * VEC; c < packed; c += THREADS * VEC) {
+          const P y = P::load(s + c);
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) f(y.get(k), c0 + c + k);
+        }
       }
-      f(xt, c0 + packed + tid, tid < tail);
+      if (tid < tail) f(xt, c0 + packed + tid);
     };
     auto put = [&](float v, int32_t place) {
       const int k = atomicAdd(&found, 1);
@@ -196,9 +203,9 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
       // the K-th largest key, bit by bit; masked logits are none
       auto count = [&](auto&& is) {
         int n = 0;
-        each([&](float v, int32_t place, bool one) {
+        each([&](float v, int32_t place) {
           const uint32_t key = key_of<T>(v);
-          n += one && key >= kLeastKey<T> && is(key, place) ? 1 : 0;
+          n += key >= kLeastKey<T> && is(key, place) ? 1 : 0;
         });
         return count_all<THREADS>(n, slot);
       };
@@ -219,9 +226,9 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
       __syncthreads();
       if (tid == 0) found = 0;
       __syncthreads();
-      each([&](float v, int32_t place, bool one) {
+      each([&](float v, int32_t place) {
         const uint32_t key = key_of<T>(v);
-        if (one && key >= kLeastKey<T> && (key > t || (key == t && place <= end))) put(v, place);
+        if (key >= kLeastKey<T> && (key > t || (key == t && place <= end))) put(v, place);
       });
       __syncthreads();
     }
@@ -231,8 +238,9 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
   }
 }
 
-// One list of K from up to `per` of a row's `lists` lists of K (each from the largest down, zeros behind).  At least K words reach the
-// largest of the lists' last ones; where too many do, the K-th largest is found bit by bit (all words but zeros differ).
+// One list of K from up to `per` of a row's `lists` lists of K (each from the largest down, zeros behind).  With m lists that have r
+// words each no smaller than some word, m r >= K, at least K words reach it: the m-th largest of the lists' r-th words, with r
+// about twice their share of K.  Where too many reach it, the K-th largest is found bit by bit (all words but zeros differ).
 constexpr int kMergeThreads = 256, kMergeEach = kMergeWords / kMergeThreads;
 struct MergeArgs {
   TopArgs a;
@@ -243,7 +251,7 @@ struct MergeArgs {
 template <typename T>
 __global__ __launch_bounds__(kMergeThreads) void top_merge_kernel(MergeArgs m) {
   __shared__ uint64_t cand[kMostCandidates];
-  __shared__ unsigned long long least;
+  __shared__ uint64_t least;
   __shared__ float slot[kMergeThreads / 64];
   __shared__ int found;
   const int tid = threadIdx.x, K = m.a.K;
@@ -254,17 +262,21 @@ __global__ __launch_bounds__(kMergeThreads) void top_merge_kernel(MergeArgs m) {
     uint64_t w[kMergeEach];
 #pragma unroll
     for (int e = 0; e < kMergeEach; ++e) w[e] = e * kMergeThreads + tid < all ? words[e * kMergeThreads + tid] : 0;
-    const uint64_t end = tid < lists ? words[tid * K + K - 1] : 0;
+    const int some = min(lists, kMergeThreads), r = min((2 * K + some - 1) / some, K), at = (K + r - 1) / r - 1;
+    const uint64_t rth = tid < some ? words[tid * K + r - 1] : 0;
     __syncthreads();
+    cand[tid] = rth;
     if (tid == 0) {
       found = 0;
       least = 1;
     }
     __syncthreads();
-    if (end > 1) atomicMax(&least, (unsigned long long)end);
+    int rank = 0;
+    for (int j = 0; j < some; ++j) rank += cand[j] > rth || (cand[j] == rth && j < tid);
+    if (tid < some && rank == at && rth > 1) least = rth;
     __syncthreads();
     uint64_t t = least;
-    auto collect = [&]() {
+    auto collect = [&]() {               // (cand is read no more: a barrier lies between)
 #pragma unroll
       for (int e = 0; e < kMergeEach; ++e)
         if (w[e] >= t) {
