@@ -93,7 +93,8 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
   constexpr int VEC = kVec<T>, WAVES = THREADS / 64;
   using P = Pack<T, VEC>;
   __shared__ uint64_t cand[kMostCandidates];
-  __shared__ uint32_t group[2 * THREADS], threshold;
+  constexpr int SHARES = 2;                                        // of a thread: 512 in all
+  __shared__ uint32_t group[SHARES * THREADS], threshold;
   __shared__ float slot[WAVES];
   __shared__ int found;
   const int tid = threadIdx.x;
@@ -147,24 +148,24 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
 
     bool exact = THREADS == 64;
     if (!exact) {
-      // two shares per thread; a pack past the last one must not count twice
-      float g0 = xt, g1 = -kInf;
+      // the largest of every share; a pack past the last one must not count twice
+      float g[SHARES];
+#pragma unroll
+      for (int e = 0; e < SHARES; ++e) g[e] = e ? -kInf : xt;
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
         float best = x[j].get(0);
 #pragma unroll
         for (int c = 1; c < VEC; ++c) best = fmaxf(best, x[j].get(c));
-        best = there(j) ? best : -kInf;
-        if (j % 2) g1 = fmaxf(g1, best);
-        else g0 = fmaxf(g0, best);
+        g[j % SHARES] = fmaxf(g[j % SHARES], there(j) ? best : -kInf);
         __builtin_amdgcn_sched_barrier(0);
       }
-      group[tid] = key_of<T>(g0);
-      group[THREADS + tid] = key_of<T>(g1);
+#pragma unroll
+      for (int e = 0; e < SHARES; ++e) group[e * THREADS + tid] = key_of<T>(g[e]);
       __syncthreads();
       if (tid < 64) {
         // the K-th largest share's maximum, from above, to 20 bits (what the others may add are few candidates more)
-        constexpr int EACH = 2 * THREADS / 64;
+        constexpr int EACH = SHARES * THREADS / 64;
         uint32_t key[EACH], t = 0;
 #pragma unroll
         for (int e = 0; e < EACH; ++e) key[e] = group[e * 64 + tid];
@@ -310,6 +311,8 @@ constexpr int64_t kMostTopBlocks = 1 << 22;
 template <typename T> hipError_t launch(const TopArgs& a, hipStream_t st) {
   const TopPlan plan = plan_top(a.rows, a.V, a.K, a.type);
   const int32_t packs = plan.cols / kVec<T>;
+  // 256 threads with up to 16 packs each: several rows on a compute unit, of which some load while others look for their threshold
+  // (7936 rows of 32000 bf16, K = 64: 120 us; 512 threads with 8 packs 140, 128 with 32 212, 1024 with 4 376)
   const dim3 grid((uint32_t)std::min((int64_t)a.rows * plan.parts, kMostTopBlocks));
   if (packs <= 64) top_kernel<T, 64, 1><<<grid, dim3(64), 0, st>>>(a, plan);
   else if (packs <= 64 * 4) top_kernel<T, 64, 4><<<grid, dim3(64), 0, st>>>(a, plan);

@@ -43,6 +43,15 @@ def test_top_logits(env, R, V, K, dtype):
     _check(env, x, min(K, 17), dtype, extra=3, offset=1)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_whose_parts_merge_in_two_steps(env, dtype):
+    """More parts than one workgroup merges at K = 256: random logits, and logits that fall so that one part has all of the largest."""
+    V = 600_001
+    x = 3.0 * np.random.default_rng(1).standard_normal((2, V))
+    x[1] = np.linspace(4.0, -4.0, V)
+    _check(env, x, 256, dtype)
+
+
 @pytest.mark.parametrize("rows", [300, 2000])
 def test_many_rows(env, rows):
     _check(env, np.random.default_rng(rows).standard_normal((rows, 300)), 11, "bfloat16")
