@@ -55,6 +55,39 @@ template <int EPT> struct Entries {
   }
 };
 
+// A row's entries by their places, in LDS: open addressing in twice as many slots as there are entries at most, and each place's shares
+// summed as whole numbers of 2^-62, whose order does not matter -- an id that comes twice takes both.
+constexpr int kSlots = 2 * kTopMax;
+struct EntryTable {
+  int32_t id[kSlots];          // -1: empty
+  unsigned long long p[kSlots];
+  template <int THREADS> __device__ __forceinline__ void clear() {
+    for (int k = threadIdx.x; k < kSlots; k += THREADS) {
+      id[k] = -1;
+      p[k] = 0;
+    }
+  }
+  __device__ static __forceinline__ uint32_t first(int32_t v) { return ((uint32_t)v * 0x9e3779b1u) >> 23; }       // of 512
+  // the slot of v, taken if there is none yet (v >= 0; K <= 256 of 512 are taken, so the search ends)
+  __device__ __forceinline__ int put(int32_t v, float share) {
+    uint32_t k = first(v);
+    for (;;) {
+      const int32_t was = atomicCAS(&id[k], -1, v);
+      if (was == -1 || was == v) break;
+      k = (k + 1) % kSlots;
+    }
+    atomicAdd(&p[k], (unsigned long long)(fmaxf(share, 0.0f) * 0x1p62f));       // (NaN: then the row's sum of exponentials is)
+    return (int)k;
+  }
+  __device__ __forceinline__ float sum(int k) const { return (float)p[k] * 0x1p-62f; }
+  __device__ __forceinline__ bool has(int32_t v) const {
+    for (uint32_t k = first(v); id[k] != -1; k = (k + 1) % kSlots)
+      if (id[k] == v) return true;
+    return false;
+  }
+};
+static_assert(kSlots == 512, "EntryTable::first");
+
 // The factors that a row's statistics give: m (the largest logit), q and r (the sums of the exponentials at tau and at 1).
 struct Factors {
   float cs, ch;        // w (1 - a), w a; zero without the term
@@ -173,8 +206,9 @@ template <typename T, int THREADS, int NP, bool TWO, bool GRAD, bool LOOP>
 __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void distill_row_kernel(DistillArgs a, int64_t rows) {
   constexpr int VEC = kVec<T>, WAVES = THREADS / 64, EPT = THREADS >= kTopMax ? 1 : kTopMax / THREADS;
   using P = Pack<T, VEC>;
-  __shared__ float red[2][6][16], p_of[kTopMax];         // (two sets in turn: a row's are read behind its barrier)
-  __shared__ int32_t id_of[kTopMax];
+  constexpr int SETS = LOOP ? 2 : 1;                       // in turn: a row's are read behind its barriers
+  __shared__ float red[SETS][6][16];
+  __shared__ EntryTable table[GRAD ? SETS : 1];
   const int tid = threadIdx.x;
   const int32_t packed = a.V / VEC * VEC, tail = a.V - packed;
   const Scales<TWO> k(a);
@@ -254,6 +288,8 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
       sl = to_float(s[max(own.label, 0)]);
       if (more) next.template load<THREADS>(a, row1);
 
+      if (GRAD) table[set].template clear<THREADS>();
+
       float um = kLowest, usum = 0.0f, ue[EPT];
 #pragma unroll
       for (int e = 0; e < EPT; ++e) um = fmaxf(um, own.u[e]);
@@ -287,15 +323,15 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
       }
 
       float term = 0.0f;
+      int slot[EPT];
       const float lq = logf(q), lu = logf(usum);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) {
-        ue[e] = exp2_fast((own.u[e] - um) * (inv_tau * kLog2e));
-        const float p = own.id[e] >= 0 ? ue[e] / usum : 0.0f;
-        if (own.id[e] >= 0) term += entry_term(p, (own.u[e] - um) * inv_tau - lu, lq, se[e] - m, inv_tau);
-        if (e * THREADS + tid < a.K) {
-          id_of[e * THREADS + tid] = own.id[e];
-          p_of[e * THREADS + tid] = p;
+        if (own.id[e] >= 0) {
+          ue[e] = exp2_fast((own.u[e] - um) * (inv_tau * kLog2e));
+          const float p = ue[e] / usum;
+          term += entry_term(p, (own.u[e] - um) * inv_tau - lu, lq, se[e] - m, inv_tau);
+          if (GRAD && f.cs != 0.0f) slot[e] = table[set].put(own.id[e], p);
         }
       }
       term = wave_all(term, Add());
@@ -344,22 +380,14 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
       if (GRAD) {
         T* grad = grad_of(row);
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-          if (f.cs != 0.0f && own.id[e] >= 0) {
-            float sum = 0.0f;
-            for (int j = 0; j < a.K; ++j) sum += id_of[j] == own.id[e] ? p_of[j] : 0.0f;
-            grad[own.id[e]] = from_float<T>(gradient_there<TWO>(se[e] - m, sum, own.id[e] == own.label, k, f, q, r));
-          }
-        }
-        if (f.ch != 0.0f && tid == THREADS - 1) {
-          bool done = false;
-          if (f.cs != 0.0f)
-            for (int j = 0; j < a.K; ++j) done |= id_of[j] == own.label;
-          if (!done) grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
-        }
+        for (int e = 0; e < EPT; ++e)
+          if (f.cs != 0.0f && own.id[e] >= 0)
+            grad[own.id[e]] = from_float<T>(gradient_there<TWO>(se[e] - m, table[set].sum(slot[e]) + (usum - usum), own.id[e] == own.label, k, f, q, r));
+        if (f.ch != 0.0f && tid == THREADS - 1 && !table[set].has(own.label))
+          grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
       }
-      // (the entries' arrays are written again behind the next row's first barrier, which every reader of them has to reach)
-      set ^= 1;
+      // (a set is written again in the row after the next one, behind a barrier that every reader has to reach)
+      set = (set + 1) % SETS;
       if (run) row = row1;
     }
     __syncthreads();
@@ -381,14 +409,13 @@ struct StreamArgs {
   float* stats;        // 4 floats per part
   float* values;       // K + 1 per row
 };
-constexpr int kStreamThreads = 512;
 
-template <typename T, bool TWO>
-__global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamArgs t) {
-  constexpr int VEC = kVec<T>, THREADS = kStreamThreads, WAVES = THREADS / 64, AHEAD = 4;
+template <typename T, int THREADS, bool TWO>
+__global__ __launch_bounds__(THREADS) void distill_stream_kernel(StreamArgs t) {
+  constexpr int VEC = kVec<T>, WAVES = THREADS / 64, AHEAD = 4;
   using P = Pack<T, VEC>;
-  __shared__ float red[6][16], p_of[kTopMax];
-  __shared__ int32_t id_of[kTopMax];
+  __shared__ float red[6][16];
+  __shared__ EntryTable table;
   const DistillArgs& a = t.a;
   const int tid = threadIdx.x;
   const Scales<TWO> k(a);
@@ -403,6 +430,7 @@ __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamAr
     own.load<THREADS>(a, row);
     own.settle(a);
     __syncthreads();                                          // (shared arrays of the unit before)
+    if (grad && t.mode != STREAM_STATS) table.clear<THREADS>();
     if (own.w == 0.0f) {
       if (t.mode != STREAM_STATS) {
         if (a.loss && tid == 0 && part == 0) a.loss[row] = 0.0f;
@@ -482,10 +510,10 @@ __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamAr
     const Factors f(a, own.w, usum != 0.0f, own.label >= 0, q, r);
     const float p = own.id[0] >= 0 ? ue / usum : 0.0f;
     float term = 0.0f;
-    if (own.id[0] >= 0) term = entry_term(p, (own.u[0] - um) * inv_tau - logf(usum), logf(q), se - m, inv_tau);
-    if (tid < a.K) {
-      id_of[tid] = own.id[0];
-      p_of[tid] = p;
+    int slot = 0;
+    if (own.id[0] >= 0) {
+      term = entry_term(p, (own.u[0] - um) * inv_tau - logf(usum), logf(q), se - m, inv_tau);
+      if (grad && f.cs != 0.0f) slot = table.put(own.id[0], p);
     }
     term = wave_all(term, Add());
     if (tid % 64 == 0) red[5][tid / 64] = term;
@@ -515,22 +543,21 @@ __global__ __launch_bounds__(kStreamThreads) void distill_stream_kernel(StreamAr
       a.loss[row] = loss;
     }
     if (grad && !f.zero) {
-      if (f.cs != 0.0f && own.id[0] >= c0 && own.id[0] < c1) {
-        float sum = 0.0f;
-        for (int j = 0; j < a.K; ++j) sum += id_of[j] == own.id[0] ? p_of[j] : 0.0f;
-        grad[own.id[0]] = from_float<T>(gradient_there<TWO>(se - m, sum, own.id[0] == own.label, k, f, q, r));
-      }
-      if (f.ch != 0.0f && tid == THREADS - 1 && own.label >= c0 && own.label < c1) {
-        bool done = false;
-        if (f.cs != 0.0f)
-          for (int j = 0; j < a.K; ++j) done |= id_of[j] == own.label;
-        if (!done) grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
-      }
+      if (f.cs != 0.0f && own.id[0] >= c0 && own.id[0] < c1)
+        grad[own.id[0]] = from_float<T>(gradient_there<TWO>(se - m, table.sum(slot) + (usum - usum), own.id[0] == own.label, k, f, q, r));
+      if (f.ch != 0.0f && tid == THREADS - 1 && own.label >= c0 && own.label < c1 && !table.has(own.label))
+        grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
     }
   }
 }
 
 constexpr int64_t kMostRowBlocks = 1 << 21;       // (a launch has fewer than 2^32 threads)
+
+template <typename T, bool TWO> void stream(const StreamArgs& t, hipStream_t st) {
+  const dim3 grid((uint32_t)std::min(t.rows * t.parts, kMostRowBlocks));
+  if (t.cols <= 256 * kVec<T> * 8) distill_stream_kernel<T, 256, TWO><<<grid, dim3(256), 0, st>>>(t);
+  else distill_stream_kernel<T, 512, TWO><<<grid, dim3(512), 0, st>>>(t);
+}
 
 template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.n * a.T;
@@ -540,15 +567,14 @@ template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& 
   // (the loss alone, of rows of more than 256 packs)
   if (plan.parts > 1 || packs > 1024 * 16 || (!GRAD && packs > 256)) {
     StreamArgs t{a, rows, plan.parts, plan.cols, STREAM_ALL, nullptr, nullptr};
-    const dim3 grid((uint32_t)std::min(rows * plan.parts, kMostRowBlocks)), block(kStreamThreads);
     if (plan.parts > 1) {
       t.stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.stats);
       t.values = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.values);
       t.mode = STREAM_STATS;
-      distill_stream_kernel<T, TWO><<<grid, block, 0, st>>>(t);
+      stream<T, TWO>(t, st);
       t.mode = STREAM_REST;
     }
-    distill_stream_kernel<T, TWO><<<grid, block, 0, st>>>(t);
+    stream<T, TWO>(t, st);
     return hipGetLastError();
   }
   // As many threads as the row needs with 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
@@ -579,9 +605,9 @@ DistillPlan plan_distill(int64_t rows, int32_t V, int32_t K, int type) {
   p.parts = 1;
   p.cols = V;
   const int32_t vec = type == TYPE_F32 ? 4 : 8;
-  // few rows of many columns: 4096 columns a part or more, up to 512 workgroups
-  if (rows > 0 && rows <= 64 && V >= 32768) {
-    const int32_t most = (int32_t)std::min<int64_t>(V / 4096, 512 / rows);
+  // few rows of many columns, or not very many of more than registers hold: 4096 columns a part or more, up to 512 workgroups
+  if (rows > 0 && ((rows <= 64 && V >= 32768) || (rows <= 256 && V / vec > 1024 * 16))) {
+    const int32_t most = (int32_t)std::min<int64_t>(V / 4096, (512 + rows - 1) / rows);
     if (most > 1) {
       p.cols = ((V + most - 1) / most + vec - 1) / vec * vec;
       p.parts = (V + p.cols - 1) / p.cols;
