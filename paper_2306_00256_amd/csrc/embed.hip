@@ -103,12 +103,15 @@ __device__ __forceinline__ void rank_keys(const uint32_t (&key)[IPT], uint32_t (
 #pragma unroll
   for (int j = 0; j < IPT; ++j) {
     const uint32_t d = key[j] >> shift & (digits - 1);
-    uint64_t same = ~0ull;
+    uint32_t lo = ~0u, hi = ~0u;               // lanes whose digit is the same, bit by bit
     for (int b = 0; b < bits; ++b) {
-      const uint64_t has = __ballot(d >> b & 1);
-      same &= d >> b & 1 ? has : ~has;
+      const uint32_t off = (d >> b & 1) - 1;   // all ones where the bit is clear
+      const uint64_t has = __ballot(off == 0);
+      lo &= (uint32_t)has ^ off;
+      hi &= (uint32_t)(has >> 32) ^ off;
     }
-    const uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+    const uint64_t same = (uint64_t)hi << 32 | lo;
+    const uint32_t before = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
     const uint32_t seen = mine[d];
     __builtin_amdgcn_wave_barrier();
     if (before == 0) mine[d] = seen + (uint32_t)__builtin_popcountll(same);
@@ -144,8 +147,8 @@ __device__ __forceinline__ void rank_keys(const uint32_t (&key)[IPT], uint32_t (
   for (int j = 0; j < IPT; ++j) to[j] += mine[key[j] >> shift & (digits - 1)];
 }
 
-// Agents' positions sorted by one workgroup each: the keys are (token, position) in one word, so that LDS holds up to 16384 of
-// them beside the counts.
+// Agents' positions sorted by one workgroup each, the keys (token, position) in one word.  (Up to 4096: with 16384, 16 a thread, it
+// takes 36 us, four launches of several workgroups each 4 to 5 us a launch.)
 template <int IPT>
 __global__ __launch_bounds__(1024) void sort_lds_kernel(EmbedArgs a, EmbedGradPlan p) {
   extern __shared__ uint32_t lds[];
@@ -428,10 +431,25 @@ __global__ __launch_bounds__(256) void few_positions_kernel(EmbedArgs a, int32_t
       for (int c = 0; c < VEC; ++c) sum[c] = 0.0f;
 #pragma unroll
       for (int k = 0; k < NT; ++k)
-        for (uint64_t m = hits[k]; m; m &= m - 1) {
-          const Pack<T, VEC> g = Pack<T, VEC>::load(G + (int64_t)(k * 64 + __builtin_ctzll(m)) * a.ldo);
+        for (uint64_t m = hits[k]; m;) {
+          // up to eight rows at once (past the last one that row again)
+          Pack<T, VEC> g[8];
+          int some = 0, at = 0;
 #pragma unroll
-          for (int c = 0; c < VEC; ++c) sum[c] += g.get(c);
+          for (int j = 0; j < 8; ++j) {
+            if (m) {
+              at = __builtin_ctzll(m);
+              m &= m - 1;
+              ++some;
+            }
+            g[j] = Pack<T, VEC>::load(G + (int64_t)(k * 64 + at) * a.ldo);
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < some) {
+#pragma unroll
+              for (int c = 0; c < VEC; ++c) sum[c] += g[j].get(c);
+            }
         }
 #pragma unroll
       for (int c = 0; c < VEC; ++c) sum[c] = ADD ? __builtin_fmaf(a.scale, sum[c], old.get(c)) : a.scale * sum[c];
@@ -501,23 +519,19 @@ hipError_t zeros(const EmbedArgs& a, hipStream_t st) {
 
 template <int IPT> hipError_t sort_lds(const EmbedArgs& a, const EmbedGradPlan& p, hipStream_t st) {
   const size_t lds = (16 * kDigits + 16 + IPT * 1024) * sizeof(uint32_t);
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sort_lds_kernel<IPT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
   sort_lds_kernel<IPT><<<dim3((uint32_t)std::min(a.n, 1 << 16)), dim3(1024), lds, st>>>(a, p);
   return hipGetLastError();
 }
 
 template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const EmbedGradPlan& p, hipStream_t st) {
-  if (p.small) return a.T <= 64 ? few_positions<T, VEC, 1>(a, st) : few_positions<T, VEC, 4>(a, st);
+  if (p.small) return a.T <= 64 ? few_positions<T, VEC, 1>(a, st) : a.T <= 256 ? few_positions<T, VEC, 4>(a, st) : few_positions<T, VEC, 16>(a, st);
   char* ws = static_cast<char*>(a.workspace);
   auto words = [&](int64_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
   uint32_t *tok = words(p.tok0), *pos = words(p.pos0);
   hipError_t e = a.accumulate ? hipSuccess : zeros(a, st);
   if (e != hipSuccess) return e;
   if (p.lds) {
-    e = a.T <= 1024 ? sort_lds<1>(a, p, st) : a.T <= 2048 ? sort_lds<2>(a, p, st) : a.T <= 4096 ? sort_lds<4>(a, p, st) : a.T <= 8192 ? sort_lds<8>(a, p, st) : sort_lds<16>(a, p, st);
+    e = a.T <= 1024 ? sort_lds<1>(a, p, st) : a.T <= 2048 ? sort_lds<2>(a, p, st) : sort_lds<4>(a, p, st);
   } else {
     uint32_t *tok2 = words(p.tok1), *pos2 = words(p.pos1);
     const dim3 grid((uint32_t)std::min((int64_t)a.n * p.tiles, kMostBlocks));

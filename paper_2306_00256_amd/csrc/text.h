@@ -26,8 +26,9 @@ struct EmbedArgs {
 
 // How the gradient's positions are brought into the order of their tokens, and its workspace.
 constexpr int kChunk = 16;             // sorted positions that one wavefront adds up
-constexpr int kSmallT = 256;           // positions per agent up to which nothing is sorted
-constexpr int kLdsT = 16384;           // ... up to which one workgroup sorts them in LDS
+constexpr int kFewT = 256, kSomeT = 1024;   // positions per agent up to which nothing is sorted: always, with few positions in all
+constexpr int kLdsT = 4096;            // ... up to which one workgroup sorts them in LDS
+constexpr int64_t kSomePositions = 4096;
 constexpr int kTile = 4096;            // positions per workgroup where several sort together
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 struct EmbedGradPlan {
@@ -40,7 +41,8 @@ struct EmbedGradPlan {
 inline int bits_of(uint32_t v) { return v ? 32 - __builtin_clz(v) : 0; }
 inline EmbedGradPlan plan_embed_grad(int64_t n, int64_t V, int64_t h, int64_t T) {
   EmbedGradPlan p{};
-  p.small = T <= kSmallT;
+  // unsorted, every position's wavefront looks through the agent's tokens
+  p.small = T <= kFewT || (T <= kSomeT && n * T * ((h + 255) / 256) <= kSomePositions);
   if (p.small) return p;
   p.bits = bits_of((uint32_t)V);       // V itself stands for padding
   p.passes = (p.bits + kDigitBits - 1) / kDigitBits;

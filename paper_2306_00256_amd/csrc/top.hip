@@ -7,6 +7,7 @@
 // last place that still belongs.  Candidates are ordered by one word of (value, place): the same result whatever the order in which
 // they were put into LDS.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_util.h"
 #include "text_util.h"
@@ -45,32 +46,50 @@ template <typename T> __device__ __forceinline__ float value_of(uint32_t key) {
 }
 template <typename T> constexpr uint32_t kLeastKey = (~(Order<T>::inf | Order<T>::sign) & Order<T>::all) + 1;    // above -inf
 
-constexpr int kMostCandidates = 1024;
+// Candidates that a workgroup's LDS holds: fewer for single wavefronts, of which a compute unit has more.
+constexpr int most_candidates(int threads) { return threads == 64 ? 512 : 1024; }
 
-// Candidates in LDS to their ranks: the K first go out, as values and places or, from a part of a row, as they are.
+// Candidates in LDS to their ranks: the K first go out, as values and places or, from a part of a row, as they are.  A thread
+// takes up to four at a time, which share what it reads.
 template <typename T, int THREADS>
 __device__ __forceinline__ void rank_and_store(const uint64_t* cand, int count, int K, float* top, int32_t* ids, uint64_t* words) {
-  for (int c = threadIdx.x; c < max(count, K); c += THREADS) {
-    if (c < count) {
-      const uint64_t own = cand[c];
-      int rank = 0;
+  constexpr int AT_ONCE = 4;
+  for (int c0 = threadIdx.x; c0 < count; c0 += THREADS * AT_ONCE) {
+    uint64_t own[AT_ONCE];
+    int rank[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      own[i] = c0 + i * THREADS < count ? cand[c0 + i * THREADS] : ~0ull;
+      rank[i] = 0;
+    }
+    if (count <= THREADS) {
 #pragma unroll 8
-      for (int j = 0; j < count; ++j) rank += cand[j] > own;
-      if (rank < K) {
-        if (words) {
-          words[rank] = own;
-        } else {
-          top[rank] = value_of<T>((uint32_t)(own >> 32));
-          ids[rank] = (int32_t)~(uint32_t)own;
-        }
+      for (int j = 0; j < count; ++j) rank[0] += cand[j] > own[0];
+    } else {
+#pragma unroll 4
+      for (int j = 0; j < count; ++j) {
+        const uint64_t other = cand[j];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) rank[i] += other > own[i];
       }
-    } else {                                                  // fewer than K that are not masked
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      if (c0 + i * THREADS >= count || rank[i] >= K) continue;
       if (words) {
-        words[c] = 0;
+        words[rank[i]] = own[i];
       } else {
-        top[c] = -kInf;
-        ids[c] = -1;
+        top[rank[i]] = value_of<T>((uint32_t)(own[i] >> 32));
+        ids[rank[i]] = (int32_t)~(uint32_t)own[i];
       }
+    }
+  }
+  for (int c = count + threadIdx.x; c < K; c += THREADS) {    // fewer than K that are not masked
+    if (words) {
+      words[c] = 0;
+    } else {
+      top[c] = -kInf;
+      ids[c] = -1;
     }
   }
 }
@@ -92,8 +111,9 @@ template <typename T, int THREADS, int NP>
 __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs a, TopPlan plan) {
   constexpr int VEC = kVec<T>, WAVES = THREADS / 64;
   using P = Pack<T, VEC>;
-  __shared__ uint64_t cand[kMostCandidates];
-  constexpr int SHARES = 2;                                        // of a thread: 512 in all
+  // shares of a thread, 512 in all where there are packs enough
+  constexpr int SHARES = THREADS > 64 ? 2 : NP < 8 ? NP : 8, MOST = most_candidates(THREADS);
+  __shared__ uint64_t cand[MOST];
   __shared__ uint32_t group[SHARES * THREADS], threshold;
   __shared__ float slot[WAVES];
   __shared__ int found;
@@ -122,33 +142,15 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
     __syncthreads();                                           // (LDS of the unit before)
     if (tid == 0) found = 0;
 
-    // f(value, place) for every logit of this thread: from the registers of a small tile, else, for the few rows that take the long
-    // way, from memory once more (kept for that, a large tile's logits would cost every row registers)
-    auto each = [&](auto&& f) {
-      if constexpr (THREADS == 64) {
-#pragma unroll
-        for (int j = 0; j < NP; ++j)
-          if (there(j)) {
-#pragma unroll
-            for (int c = 0; c < VEC; ++c) f(x[j].get(c), c0 + (int32_t)(at(j) / sizeof(T)) + c);
-          }
-      } else {
-        for (int32_t c = tid * VEC; c < packed; c += THREADS * VEC) {
-          const P y = P::load(s + c);
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) f(y.get(k), c0 + c + k);
-        }
-      }
-      if (tid < tail) f(xt, c0 + packed + tid);
-    };
-    auto put = [&](float v, int32_t place) {
+    const uint32_t key_t = key_of<T>(xt);
+    auto put = [&](uint32_t key, int32_t place) {
       const int k = atomicAdd(&found, 1);
-      if (k < kMostCandidates) cand[k] = (uint64_t)key_of<T>(v) << 32 | (uint32_t)~place;
+      if (k < MOST) cand[k] = (uint64_t)key << 32 | (uint32_t)~place;
     };
 
-    bool exact = THREADS == 64;
-    if (!exact) {
-      // the largest of every share; a pack past the last one must not count twice
+    // the largest of every share; a pack past the last one must not count twice
+    uint32_t t = 0;
+    {
       float g[SHARES];
 #pragma unroll
       for (int e = 0; e < SHARES; ++e) g[e] = e ? -kInf : xt;
@@ -160,27 +162,46 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
         g[j % SHARES] = fmaxf(g[j % SHARES], there(j) ? best : -kInf);
         __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int e = 0; e < SHARES; ++e) group[e * THREADS + tid] = key_of<T>(g[e]);
-      __syncthreads();
-      if (tid < 64) {
-        // the K-th largest share's maximum, from above, to 20 bits (what the others may add are few candidates more)
-        constexpr int EACH = SHARES * THREADS / 64;
-        uint32_t key[EACH], t = 0;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) key[e] = group[e * 64 + tid];
+      // the K-th largest of them, from above, to 20 bits (what the others may add are few candidates more), by one wavefront
+      auto search = [&](auto&& key, auto each) {
         for (int bit = kBits<T> - 1; bit >= std::max(kBits<T> - 20, 0); --bit) {
           const uint32_t t1 = t | 1u << bit;
           int n = 0;
 #pragma unroll
-          for (int e = 0; e < EACH; ++e) n += __builtin_popcountll(__ballot(key[e] >= t1));
+          for (int e = 0; e < decltype(each)::value; ++e) n += __builtin_popcountll(__ballot(key[e] >= t1));
           if (n >= a.K) t = t1;
           if (n == a.K) break;
         }
-        if (tid == 0) threshold = max(t, kLeastKey<T>);
+      };
+      if constexpr (WAVES == 1) {
+        uint32_t key[SHARES];
+#pragma unroll
+        for (int e = 0; e < SHARES; ++e) key[e] = key_of<T>(g[e]);
+        search(key, std::integral_constant<int, SHARES>());
+        __syncthreads();
+      } else {
+#pragma unroll
+        for (int e = 0; e < SHARES; ++e) group[e * THREADS + tid] = key_of<T>(g[e]);
+        __syncthreads();
+        if (tid < 64) {
+          constexpr int EACH = SHARES * THREADS / 64;
+          uint32_t key[EACH];
+#pragma unroll
+          for (int e = 0; e < EACH; ++e) key[e] = group[e * 64 + tid];
+          search(key, std::integral_constant<int, EACH>());
+          if (tid == 0) threshold = t;
+        }
+        __syncthreads();
+        t = threshold;
       }
+    }
+    // (from a small tile the long way is shorter than ranking many: taken at once where fewer shares than K were found to hold any)
+    constexpr bool KEPT = THREADS == 64 && NP <= 4;
+    if (KEPT && t == 0 && cols > kTopMax) {
+      if (tid == 0) found = kTopMax + 1;
       __syncthreads();
-      const float least = value_of<T>(threshold);
+    } else {
+      const float least = value_of<T>(max(t, kLeastKey<T>));
       asm volatile("" : "+v"(mine));
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
@@ -192,34 +213,62 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
           x[j].again();
 #pragma unroll
           for (int c = 0; c < VEC; ++c)
-            if (!(x[j].get(c) < least)) put(x[j].get(c), c0 + (int32_t)(at(j) / sizeof(T)) + c);
+            if (!(x[j].get(c) < least)) put(key_of<T>(x[j].get(c)), c0 + (int32_t)(at(j) / sizeof(T)) + c);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (tid < tail && !(xt < least)) put(xt, c0 + packed + tid);
+      if (tid < tail && !(xt < least)) put(key_t, c0 + packed + tid);
       __syncthreads();
-      exact = found > kMostCandidates;
     }
-    if (exact) {
+    if (found > (KEPT ? kTopMax : MOST)) {
+      // f(key, place) for every logit of this thread: from the keys of a small tile, else from memory once more (kept for the few rows
+      // that come here, a large tile's logits would cost every row registers); 0 stands for none
+      uint32_t key[KEPT ? NP * VEC : 1];
+      if constexpr (KEPT) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+#pragma unroll
+          for (int c = 0; c < VEC; ++c) key[j * VEC + c] = there(j) ? key_of<T>(x[j].get(c)) : 0;
+      }
+      auto each = [&](auto&& f) {
+        if constexpr (KEPT) {
+#pragma unroll
+          for (int j = 0; j < NP; ++j)
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) f(key[j * VEC + c], c0 + (int32_t)(at(j) / sizeof(T)) + c);
+        } else {
+          for (int32_t c = tid * VEC; c < packed; c += THREADS * VEC) {
+            const P y = P::load(s + c);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) f(key_of<T>(y.get(k)), c0 + c + k);
+          }
+        }
+        f(key_t, c0 + packed + tid);
+      };
       // the K-th largest key, bit by bit; masked logits are none
       auto count = [&](auto&& is) {
         int n = 0;
-        each([&](float v, int32_t place) {
-          const uint32_t key = key_of<T>(v);
-          n += key >= kLeastKey<T> && is(key, place) ? 1 : 0;
-        });
+        each([&](uint32_t key, int32_t place) { n += is(key, place) ? 1 : 0; });
         return count_all<THREADS>(n, slot);
       };
-      uint32_t t = 0;
+      t = 0;
+      int reach = 0;                                           // logits that reach it
       for (int bit = kBits<T> - 1; bit >= 0; --bit) {
         const uint32_t t1 = t | 1u << bit;
-        if (count([&](uint32_t key, int32_t) { return key >= t1; }) >= a.K) t = t1;
+        const int n = count([&](uint32_t key, int32_t) { return key >= max(t1, kLeastKey<T>); });
+        if (n >= a.K) {
+          t = t1;
+          reach = n;
+        }
+        if (n == a.K) break;                                   // just these
       }
-      // how many of its equals belong, and the place of the last of them (t = 0: fewer than K logits, all belong)
-      const int need = a.K - count([&](uint32_t key, int32_t) { return key > t; });
-      int32_t end = 0;
-      if (t != 0) {
-        for (int bit = 30 - __builtin_clz((uint32_t)a.V | 1) + 1; bit >= 0; --bit) {
+      t = max(t, kLeastKey<T>);
+      // more than K: how many of the K-th's equals belong, and the place of the last of them
+      int32_t end = 0x7fffffff;
+      if (reach > a.K) {
+        const int need = a.K - count([&](uint32_t key, int32_t) { return key > t; });
+        end = 0;
+        for (int bit = 31 - __builtin_clz((uint32_t)a.V | 1); bit >= 0; --bit) {
           const int32_t end1 = end + (1 << bit);
           if (count([&](uint32_t key, int32_t place) { return key == t && place < end1; }) < need) end = end1;
         }
@@ -227,15 +276,14 @@ __global__ __launch_bounds__(THREADS, NP == 16 ? 4 : 1) void top_kernel(TopArgs 
       __syncthreads();
       if (tid == 0) found = 0;
       __syncthreads();
-      each([&](float v, int32_t place) {
-        const uint32_t key = key_of<T>(v);
-        if (key >= kLeastKey<T> && (key > t || (key == t && place <= end))) put(v, place);
+      each([&](uint32_t key, int32_t place) {
+        if (key > t || (key == t && place <= end)) put(key, place);
       });
       __syncthreads();
     }
     float* top = a.top + row * a.K;
     int32_t* ids = a.ids + row * a.K;
-    rank_and_store<T, THREADS>(cand, min(found, kMostCandidates), a.K, top, ids, plan.parts > 1 ? static_cast<uint64_t*>(a.workspace) + unit * a.K : nullptr);
+    rank_and_store<T, THREADS>(cand, min(found, MOST), a.K, top, ids, plan.parts > 1 ? static_cast<uint64_t*>(a.workspace) + unit * a.K : nullptr);
   }
 }
 
@@ -251,7 +299,8 @@ struct MergeArgs {
 };
 template <typename T>
 __global__ __launch_bounds__(kMergeThreads) void top_merge_kernel(MergeArgs m) {
-  __shared__ uint64_t cand[kMostCandidates];
+  constexpr int MOST = most_candidates(kMergeThreads);
+  __shared__ uint64_t cand[MOST];
   __shared__ uint64_t least;
   __shared__ float slot[kMergeThreads / 64];
   __shared__ int found;
@@ -282,12 +331,12 @@ __global__ __launch_bounds__(kMergeThreads) void top_merge_kernel(MergeArgs m) {
       for (int e = 0; e < kMergeEach; ++e)
         if (w[e] >= t) {
           const int k = atomicAdd(&found, 1);
-          if (k < kMostCandidates) cand[k] = w[e];
+          if (k < MOST) cand[k] = w[e];
         }
       __syncthreads();
     };
     collect();
-    if (found > kMostCandidates) {
+    if (found > MOST) {
       t = 0;
       for (int bit = 31 + kBits<T>; bit >= 0; --bit) {
         const uint64_t t1 = t | 1ull << bit;
@@ -302,7 +351,7 @@ __global__ __launch_bounds__(kMergeThreads) void top_merge_kernel(MergeArgs m) {
       __syncthreads();
       collect();
     }
-    rank_and_store<T, kMergeThreads>(cand, min(found, kMostCandidates), K, m.a.top + row * K, m.a.ids + row * K, m.out ? m.out + unit * K : nullptr);
+    rank_and_store<T, kMergeThreads>(cand, min(found, MOST), K, m.a.top + row * K, m.a.ids + row * K, m.out ? m.out + unit * K : nullptr);
   }
 }
 
@@ -312,11 +361,15 @@ template <typename T> hipError_t launch(const TopArgs& a, hipStream_t st) {
   const TopPlan plan = plan_top(a.rows, a.V, a.K, a.type);
   const int32_t packs = plan.cols / kVec<T>;
   // 256 threads with up to 16 packs each: several rows on a compute unit, of which some load while others look for their threshold
-  // (7936 rows of 32000 bf16, K = 64: 120 us; 512 threads with 8 packs 140, 128 with 32 212, 1024 with 4 376)
+  // (7936 rows of 32000 bf16, K = 64: 120 us; 512 threads with 8 packs 140, 128 with 32 212, 1024 with 4 376).  Longer rows
+  // in parts: 1000 rows of 33216 fp32, K = 157, 67 us, in one tile of 512 threads 89.  Many short rows by a wavefront each, which
+  // needs no barriers (87219 rows of 2304 bf16, K = 6: 218 us, by 256 threads 313); few of them are done sooner by more threads.
   const dim3 grid((uint32_t)std::min((int64_t)a.rows * plan.parts, kMostTopBlocks));
   if (packs <= 64) top_kernel<T, 64, 1><<<grid, dim3(64), 0, st>>>(a, plan);
   else if (packs <= 64 * 4) top_kernel<T, 64, 4><<<grid, dim3(64), 0, st>>>(a, plan);
-  else if (packs <= 256 * 4) top_kernel<T, 256, 4><<<grid, dim3(256), 0, st>>>(a, plan);
+  else if (packs <= 256 * 4 && grid.x <= 2048) top_kernel<T, 256, 4><<<grid, dim3(256), 0, st>>>(a, plan);
+  else if (packs <= 64 * 8) top_kernel<T, 64, 8><<<grid, dim3(64), 0, st>>>(a, plan);
+  else if (packs <= 64 * 16) top_kernel<T, 64, 16><<<grid, dim3(64), 0, st>>>(a, plan);
   else if (packs <= 256 * 8) top_kernel<T, 256, 8><<<grid, dim3(256), 0, st>>>(a, plan);
   else top_kernel<T, 256, 16><<<grid, dim3(256), 0, st>>>(a, plan);
   uint64_t *in = static_cast<uint64_t*>(a.workspace), *out = in + plan.second / 8;
@@ -336,9 +389,10 @@ template <typename T> hipError_t launch(const TopArgs& a, hipStream_t st) {
 TopPlan plan_top(int64_t rows, int32_t V, int32_t K, int type) {
   TopPlan p{};
   const int32_t vec = type == TYPE_F32 ? 4 : 8, most = 256 * 16 * vec;     // columns of the largest register tile
-  // parts that registers hold; few rows in parts of 4096 columns or more, up to 1024 workgroups and one merge
+  // parts that registers hold; few rows of more than 32768 columns in parts of 4096 or more, up to 1024 workgroups and one merge
+  // (64 rows of 84864 bf16: parts of 4096 17.0 us, of 32768 20.0; 286 rows of 28571: in one 12.2 us, in parts 14.8)
   int64_t parts = (V + (int64_t)most - 1) / most;
-  if (rows > 0) parts = std::max(parts, std::min<int64_t>({V / 4096, 1024 / rows, kMergeWords / K}));
+  if (rows > 0 && V > 32768) parts = std::max(parts, std::min<int64_t>({V / 4096, 1024 / rows, kMergeWords / K}));
   parts = std::max<int64_t>(parts, 1);
   p.cols = (int32_t)(((V + parts - 1) / parts + vec - 1) / vec * vec);
   p.parts = (V + p.cols - 1) / p.cols;
