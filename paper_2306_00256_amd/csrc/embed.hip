@@ -191,7 +191,7 @@ __global__ __launch_bounds__(1024) void sort_lds_kernel(EmbedArgs a, EmbedGradPl
   }
 }
 
-// Longer sequences: tiles of kTile positions, one pass of kDigitBits bits in two launches.  Counts of every tile first ...
+// Longer sequences: tiles of 1024 IPT positions, one pass of kDigitBits bits in two launches.  Counts of every tile first ...
 struct PassArgs {
   const int32_t* tokens;       // first pass, else null
   const uint32_t *tok, *pos;   // later passes
@@ -203,7 +203,8 @@ __device__ __forceinline__ uint32_t pass_key(const PassArgs& p, int64_t i, int64
   const int32_t v = p.tokens[i * p.T + t];
   return (uint32_t)(v >= 0 && v < p.V ? v : p.V);
 }
-__global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p) {
+template <int IPT> __global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p) {
+  constexpr int kTile = 1024 * IPT;
   __shared__ uint32_t count[kDigits];
   const int64_t sorts = (int64_t)p.n * p.tiles;
   for (int64_t b = blockIdx.x; b < sorts; b += gridDim.x) {
@@ -218,8 +219,8 @@ __global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p) {
   }
 }
 // ... then every tile's keys to their places: behind the smaller digits of all tiles and the same digit's of earlier tiles.
-__global__ __launch_bounds__(1024) void place_keys_kernel(PassArgs p) {
-  constexpr int IPT = kTile / 1024;
+template <int IPT> __global__ __launch_bounds__(1024) void place_keys_kernel(PassArgs p) {
+  constexpr int kTile = 1024 * IPT;
   __shared__ uint32_t count[16 * kDigits], totals[16], base[kDigits], sums[16];
   const int64_t sorts = (int64_t)p.n * p.tiles;
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
@@ -227,12 +228,14 @@ __global__ __launch_bounds__(1024) void place_keys_kernel(PassArgs p) {
     const int64_t i = b / p.tiles;
     const int32_t tile = (int32_t)(b - i * p.tiles);
     uint32_t before = 0, all = 0;
-    if (tid < kDigits)
+    if (tid < kDigits) {
+#pragma unroll 8
       for (int32_t k = 0; k < p.tiles; ++k) {
         const uint32_t c = p.hist[(i * p.tiles + k) * kDigits + tid];
         all += c;
         before += k < tile ? c : 0;
       }
+    }
     uint32_t upto = all;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -346,7 +349,8 @@ __global__ __launch_bounds__(256) void walk_kernel(WalkArgs w) {
   }
 }
 
-// One wavefront per chunk and tile of columns: the token that begins in the chunk and goes on behind it.
+// One wavefront per chunk and tile of columns: the token that begins in the chunk and goes on behind it.  (Four
+// wavefronts that share the chunks of a frequent token were slower: 14066 positions of 727 tokens 21 us, 14 this way.)
 template <int VEC, bool ADD>
 __global__ __launch_bounds__(256) void join_kernel(WalkArgs w) {
   const EmbedArgs& a = w.e;
@@ -372,7 +376,7 @@ __global__ __launch_bounds__(256) void join_kernel(WalkArgs w) {
       // chunks that begin with the token: a run of them, its end by ballot
       const uint64_t mine = __ballot(c + lane < w.chunks && tok[(int64_t)min(c + lane, w.chunks - 1) * kChunk] == v);
       const int32_t run = mine == ~0ull ? 64 : __builtin_ctzll(~mine);
-      constexpr int kAhead = 8;
+      constexpr int kAhead = 16;
       for (int32_t k0 = 0; k0 < run; k0 += kAhead) {
         Pack<float, VEC> p[kAhead];
 #pragma unroll
@@ -538,8 +542,13 @@ template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const Emb
     for (int k = 0; k < p.passes && e == hipSuccess; ++k) {
       const PassArgs q{k ? nullptr : a.tokens, tok, pos, tok2, pos2, words(p.hist), a.n, a.V, a.T, p.tiles, k * p.digit_bits,
                        std::min(p.digit_bits, p.bits - k * p.digit_bits)};
-      count_digits_kernel<<<grid, dim3(1024), 0, st>>>(q);
-      place_keys_kernel<<<grid, dim3(1024), 0, st>>>(q);
+      if (tile_of_sort(a.T) == 1024) {
+        count_digits_kernel<1><<<grid, dim3(1024), 0, st>>>(q);
+        place_keys_kernel<1><<<grid, dim3(1024), 0, st>>>(q);
+      } else {
+        count_digits_kernel<4><<<grid, dim3(1024), 0, st>>>(q);
+        place_keys_kernel<4><<<grid, dim3(1024), 0, st>>>(q);
+      }
       e = hipGetLastError();
       std::swap(tok, tok2);
       std::swap(pos, pos2);

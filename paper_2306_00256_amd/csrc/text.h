@@ -29,7 +29,8 @@ constexpr int kChunk = 16;             // sorted positions that one wavefront ad
 constexpr int kFewT = 256, kSomeT = 1024;   // positions per agent up to which nothing is sorted: always, with few positions in all
 constexpr int kLdsT = 4096;            // ... up to which one workgroup sorts them in LDS
 constexpr int64_t kSomePositions = 4096;
-constexpr int kTile = 4096;            // positions per workgroup where several sort together
+// Positions per workgroup where several sort together: 1024, one a thread, while few workgroups have to add up the others' counts.
+constexpr int tile_of_sort(int64_t T) { return T <= (1 << 16) ? 1024 : 4096; }
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 struct EmbedGradPlan {
   bool small, lds;
@@ -50,7 +51,7 @@ inline EmbedGradPlan plan_embed_grad(int64_t n, int64_t V, int64_t h, int64_t T)
   p.pos_bits = bits_of((uint32_t)(T - 1));
   p.lds = T <= kLdsT && p.bits + p.pos_bits <= 32;
   p.chunks = (int32_t)((T + kChunk - 1) / kChunk);
-  p.tiles = p.lds ? 1 : (int32_t)((T + kTile - 1) / kTile);
+  p.tiles = p.lds ? 1 : (int32_t)((T + tile_of_sort(T) - 1) / tile_of_sort(T));
   p.pitch = (h + 3) / 4 * 4;
   auto take = [&](int64_t bytes) { const int64_t at = p.bytes; p.bytes += (bytes + 255) / 256 * 256; return at; };
   p.tok0 = take(n * T * 4);
