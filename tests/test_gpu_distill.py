@@ -145,6 +145,16 @@ def test_many_rows(env, rows):
     _check(env, "bfloat16", logits, top, ids, labels, weight, None, 2.0, 0.5)
 
 
+# many rows that take a whole compute unit's registers (a workgroup loops over them), rows of padding among them, and longer ones
+@pytest.mark.parametrize("dtype,rows,V", [("float32", 530, 32777), ("bfloat16", 530, 65545), ("float16", 300, 70001), ("bfloat16", 257, 131080), ("float32", 260, 65541)])
+@pytest.mark.parametrize("hard", [0.0, 0.5])
+def test_many_long_rows(env, dtype, rows, V, hard):
+    logits, top, ids, labels, weight = _case(rows, 1, V, 8, rows)
+    labels[::7] = -1
+    ids[::5] = -1
+    _check(env, dtype, logits, top, ids, labels, weight, None, 2.0, hard)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V", [300, 70000])
 def test_cross_entropy_alone(env, dtype, V):

@@ -101,7 +101,8 @@ def test_gradient(env, n, T, V, h, off, tail, extra, dtype, accumulate):
 # rows than there are positions
 @pytest.mark.parametrize("n,T,V,h", [(1, 31, 5, 8), (2, 32, 1, 8), (2, 33, 2, 8), (1, 63, 70000, 4), (3, 127, 9, 20), (1, 128, 257, 16), (2, 129, 300, 64), (1, 511, 13, 68),
                                      (1, 1023, 100, 12), (2, 1025, 40000, 8), (1, 2049, 600, 36), (5, 4097, 1000, 16), (1, 8191, 3000, 8), (2, 8193, 131072, 4), (1, 16385, 131073, 4),
-                                     (1, 20000, 300000, 4), (2, 40000, 50, 8)])
+                                     (1, 20000, 300000, 4), (2, 40000, 50, 8), (1, 70000, 300, 4), (1, 2100, 2_100_000, 2),
+                                     (3, 256, 90, 300), (20, 257, 90, 8), (4, 1024, 33, 8), (5, 1024, 33, 260), (3, 4096, 1000, 8)])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_gradient_at_the_ends_of_tiles(env, n, T, V, h, accumulate):
     tokens = tokens_of(np.random.default_rng(T + 1), n, T, V)

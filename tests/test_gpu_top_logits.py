@@ -58,6 +58,25 @@ def test_many_rows(env, rows):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V,K", [(1300, 200), (2500, 64), (3500, 256), (8100, 256)])
+def test_many_rows_of_some_columns(env, V, K, dtype):
+    """2100 rows, 21 of them again and again, some equal everywhere or masked."""
+    torch, P = env
+    x = 3.0 * np.random.default_rng(V).standard_normal((21, V))
+    x[3] = 1.0
+    x[5, 10:] = -np.inf
+    x[6, ::3] = 2.0
+    x[8, 5] = np.nan
+    dev, x64 = stored(torch, x, dtype)
+    rows = dev.repeat(100, 1)
+    top, ids = torch.full((2100, K), 4.5, device="cuda"), torch.full((2100, K), -9, dtype=torch.int32, device="cuda")
+    P.ceca_top_logits(rows, 2100, V, K, top, ids)
+    values, places = OT.top_logits(x64, K)
+    assert np.array_equal(ids.cpu().numpy(), np.tile(places, (100, 1)))
+    assert np.array_equal(top.double().cpu().numpy(), np.tile(values, (100, 1)), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V", [100, 5000, 70001])
 @pytest.mark.parametrize("K", [1, 64, 256])
 def test_ties_order_and_masks(env, V, K, dtype):
