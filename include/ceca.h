@@ -321,7 +321,8 @@ int32_t ceca_graph_rounds(const float* X_in, float* X_out, int32_t n, int64_t d,
  * computed in fp32 and rounded once, to nearest even, where a result is stored in 16 bits.  The results of a call depend on
  * its arguments alone: no floating-point atomics are used.  Pointers lie on their element type's boundary (CECA_EINVAL
  * otherwise); pitches are counted in elements.  n T, the number of positions, is below 2^31; T = 0 does nothing (and
- * ceca_embed_grad then sees no token). */
+ * ceca_embed_grad then sees no token).  A workspace serves one call at a time: calls that may overlap (other streams, graphs that
+ * are replayed side by side) need one each. */
 enum { CECA_F32 = 0, CECA_BF16 = 1, CECA_F16 = 2 };
 
 /* Embedding lookup: out row i T + t = scale * row tokens[i T + t] of agent i's table, i < n, t < T.

@@ -361,9 +361,8 @@ __global__ __launch_bounds__(256) void join_kernel(WalkArgs w) {
     const int32_t chunk = (int32_t)(ic - i * (w.chunks - 1));
     const uint32_t* tok = w.tok + i * a.T;
     const int32_t end = (chunk + 1) * kChunk;            // a place there is: this is not the last chunk
-    const uint32_t v = tok[end - 1];
-    if (v >= (uint32_t)a.V || tok[end] != v) continue;
-    if (chunk > 0 && tok[chunk * kChunk - 1] == v) continue;    // it began earlier
+    const uint32_t v = tok[end - 1], next = tok[end], before = tok[max(chunk * kChunk - 1, 0)];       // (at once: a wait each would triple it)
+    if (v >= (uint32_t)a.V || next != v || (chunk > 0 && before == v)) continue;     // no token, or done, or begun earlier
     const Columns<VEC> col((int32_t)(unit - ic * w.tiles) * 64 * VEC + lane * VEC, a.h);
     const float* part = w.partial + (i * w.chunks + chunk) * 2 * w.pitch;
     float sum[VEC];
@@ -490,7 +489,7 @@ uint32_t four_a_block(int64_t units) { return (uint32_t)std::min((units + 3) / 4
 template <typename T, int VEC> hipError_t lookup(const EmbedArgs& a, hipStream_t st) {
   const int32_t tiles = (a.h + 64 * VEC - 1) / (64 * VEC);
   const int64_t rows = (int64_t)a.n * a.T;
-  // four positions a wavefront once there are wavefronts enough
+  // four positions a wavefront once there are wavefronts enough (31 x 2048 positions of 512 bf16: 31.2 us, with two 33.5, eight 33.6)
   if (rows * tiles >= 1 << 14) embed_kernel<T, VEC, 4><<<dim3(four_a_block((rows + 3) / 4 * tiles)), dim3(256), 0, st>>>(a, tiles);
   else embed_kernel<T, VEC, 1><<<dim3(four_a_block(rows * tiles)), dim3(256), 0, st>>>(a, tiles);
   return hipGetLastError();

@@ -389,10 +389,10 @@ template <typename T> hipError_t launch(const TopArgs& a, hipStream_t st) {
 TopPlan plan_top(int64_t rows, int32_t V, int32_t K, int type) {
   TopPlan p{};
   const int32_t vec = type == TYPE_F32 ? 4 : 8, most = 256 * 16 * vec;     // columns of the largest register tile
-  // parts that registers hold; few rows of more than 32768 columns in parts of 4096 or more, up to 1024 workgroups and one merge
+  // parts that registers hold; few rows of more than 32768 columns in parts of about 4096, up to 1024 workgroups and one merge
   // (64 rows of 84864 bf16: parts of 4096 17.0 us, of 32768 20.0; 286 rows of 28571: in one 12.2 us, in parts 14.8)
   int64_t parts = (V + (int64_t)most - 1) / most;
-  if (rows > 0 && V > 32768) parts = std::max(parts, std::min<int64_t>({V / 4096, 1024 / rows, kMergeWords / K}));
+  if (rows > 0 && V > 32768) parts = std::max(parts, std::min<int64_t>({(V + 4095) / 4096, 1024 / rows, kMergeWords / K}));
   parts = std::max<int64_t>(parts, 1);
   p.cols = (int32_t)(((V + parts - 1) / parts + vec - 1) / vec * vec);
   p.parts = (V + p.cols - 1) / p.cols;
