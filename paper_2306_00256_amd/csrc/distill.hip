@@ -398,7 +398,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
 // ---- rows that stream through ----
 // Longer rows than registers hold: a workgroup reads the row twice, the second time mostly from the last-level cache.  The loss alone
 // needs a row once and no registers to keep it in: more workgroups, more loads in flight (975 rows of 50021 fp16 28.4 us,
-// from a register tile 32.8).  Few rows:
+// from a register tile 32.8; four packs a thread at once: with more, or as a ring, the registers cost more than it gains).  Few rows:
 // `parts` workgroups take a row's columns; one launch leaves each part's maximum and sums in the workspace (and the logits at the
 // entries' places, which the gradient may overwrite), a second one joins them and does the rest.
 enum StreamMode : int { STREAM_ALL = 0, STREAM_STATS = 1, STREAM_REST = 2 };
@@ -580,7 +580,7 @@ template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& 
   // As many threads as the row needs with 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
   // unit, of which some load while others compute: one row each (7936 rows of 32000 bf16, two softmaxes 206 us; looping, with the
   // next row's loads in between, 242).  Rows of 1024 threads have the compute unit to themselves and loop (15872 rows of
-  // 128000 bf16 1605 us; loads between the rows 1840).
+  // 128000 bf16 1507 us, 5.1 TB/s; with the loads between the rows it took 230 us more).
   if (packs <= 64) distill_row_kernel<T, 64, 1, TWO, GRAD, false><<<blocks, dim3(64), 0, st>>>(a, rows);
   else if (packs <= 64 * 4) distill_row_kernel<T, 64, 4, TWO, GRAD, false><<<blocks, dim3(64), 0, st>>>(a, rows);
   else if constexpr (GRAD) {
