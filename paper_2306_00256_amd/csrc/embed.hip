@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int32_t tiles) 
 // ---- the gradient ----
 // e_i[v, :] = scale * sum of G's rows at v's positions.  A position's row is read once, a table's row is written once: what bounds
 // it is the memory's rate, mostly for the zeros of rows whose tokens do not occur.  Four launches:
-//   zeros  over the tables (not where the sums are added to what is there)
+//   zeros  over the tables (not where the sums are added to what is there; few of them go with the sort)
 //   sort   positions into the order of (token, position), in LDS
 //   walk   a wavefront adds the rows of kChunk sorted positions up, in order; where a token's positions lie in one chunk its row
 //          of the table is done, else the chunk's share goes to the workspace
@@ -71,15 +71,21 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int32_t tiles) 
 // One 16-byte store per thread and short-lived workgroups in the order of memory are the fastest way to write zeros: 2 GB at 6.8
 // TB/s, 6.0 with two stores, 5.6 to 6.1 with four and more or 1024 threads, 4.5 to 5.8 with long-lived workgroups that sweep
 // memory together.  `all` workgroups' shares, `blocks` per piece of `count` floats, `pitch` apart.
-__global__ __launch_bounds__(256) void zeros_kernel(float* p, int64_t count, int64_t pitch, uint32_t blocks, uint32_t all) {
-  for (uint64_t b = blockIdx.x; b < all; b += gridDim.x) {
-    const uint32_t i = blocks == all ? 0 : (uint32_t)b / blocks;
-    const int64_t at = (int64_t)((uint32_t)b - i * blocks) * 1024 + threadIdx.x * 4;
-    float* q = p + i * pitch;
-    if (at + 4 <= count) st_plain<vf4>(q + at, vf4{0.0f, 0.0f, 0.0f, 0.0f});
-    else
-      for (int64_t k = at; k < count; ++k) q[k] = 0.0f;
-  }
+struct ZeroArgs {
+  float* p;
+  int64_t count, pitch;
+  uint32_t blocks, all;
+};
+template <int THREADS> __device__ __forceinline__ void write_zeros(const ZeroArgs& z, uint32_t b) {
+  const uint32_t i = z.blocks == z.all ? 0 : b / z.blocks;
+  const int64_t at = (int64_t)(b - i * z.blocks) * (4 * THREADS) + threadIdx.x * 4;
+  float* q = z.p + i * z.pitch;
+  if (at + 4 <= z.count) st_plain<vf4>(q + at, vf4{0.0f, 0.0f, 0.0f, 0.0f});
+  else
+    for (int64_t k = at; k < z.count; ++k) q[k] = 0.0f;
+}
+__global__ __launch_bounds__(256) void zeros_kernel(ZeroArgs z) {
+  for (uint64_t b = blockIdx.x; b < z.all; b += gridDim.x) write_zeros<256>(z, (uint32_t)b);
 }
 // The same where something lies between the rows: a wavefront per row.
 __global__ __launch_bounds__(256) void zero_rows_kernel(EmbedArgs a) {
@@ -147,16 +153,20 @@ __device__ __forceinline__ void rank_keys(const uint32_t (&key)[IPT], uint32_t (
   for (int j = 0; j < IPT; ++j) to[j] += mine[key[j] >> shift & (digits - 1)];
 }
 
-// Agents' positions sorted by one workgroup each, the keys (token, position) in one word.  (Up to 4096: with 16384, 16 a thread, it
-// takes 36 us, four launches of several workgroups each 4 to 5 us a launch.)
+// Agents' positions sorted by one workgroup each, the keys (token, position) in one word.  (Up to 8192: 75 x 4524 positions of 32
+// fp16 106 us, sorted by five workgroups each 124; 16384 would take 36 us alone, two passes of two launches 24.)
 template <int IPT>
-__global__ __launch_bounds__(1024) void sort_lds_kernel(EmbedArgs a, EmbedGradPlan p) {
+__global__ __launch_bounds__(1024) void sort_lds_kernel(EmbedArgs a, EmbedGradPlan p, ZeroArgs z, uint32_t sorts) {
+  if (blockIdx.x >= sorts) {
+    write_zeros<1024>(z, blockIdx.x - sorts);
+    return;
+  }
   extern __shared__ uint32_t lds[];
   uint32_t* count = lds;                               // 16 x digits
   uint32_t* totals = lds + 16 * kDigits;
   uint32_t* keys = totals + 16;                        // IPT * 1024
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
+  for (int64_t i = blockIdx.x; i < a.n; i += sorts) {
     const int32_t* tokens = a.tokens + i * a.T;
     uint32_t key[IPT], to[IPT];
     const uint32_t none = (uint32_t)((((uint64_t)1 << (p.bits + p.pos_bits)) - 1));
@@ -203,11 +213,15 @@ __device__ __forceinline__ uint32_t pass_key(const PassArgs& p, int64_t i, int64
   const int32_t v = p.tokens[i * p.T + t];
   return (uint32_t)(v >= 0 && v < p.V ? v : p.V);
 }
-template <int IPT> __global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p) {
+template <int IPT> __global__ __launch_bounds__(1024) void count_digits_kernel(PassArgs p, ZeroArgs z, uint32_t counts) {
+  if (blockIdx.x >= counts) {
+    write_zeros<1024>(z, blockIdx.x - counts);
+    return;
+  }
   constexpr int kTile = 1024 * IPT;
   __shared__ uint32_t count[kDigits];
   const int64_t sorts = (int64_t)p.n * p.tiles;
-  for (int64_t b = blockIdx.x; b < sorts; b += gridDim.x) {
+  for (int64_t b = blockIdx.x; b < sorts; b += counts) {
     const int64_t i = b / p.tiles, t0 = (b - i * p.tiles) * kTile;
     if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
     __syncthreads();
@@ -508,21 +522,37 @@ template <typename T, int VEC, int NT> hipError_t few_positions(const EmbedArgs&
   return hipGetLastError();
 }
 
+// The zeros of all tables for workgroups of `floats` floats: one piece where nothing lies between the tables, else one per table
+// (fewer than 2^43 bytes: workgroups fit 32 bits).
+ZeroArgs zero_args(const EmbedArgs& a, int64_t floats) {
+  const bool whole = a.n == 1 || a.lde == (int64_t)a.V * a.h;
+  const int64_t count = (whole ? a.n : 1) * (int64_t)a.V * a.h, blocks = (count + floats - 1) / floats;
+  return ZeroArgs{a.dE, count, a.lde, (uint32_t)blocks, (uint32_t)(blocks * (whole ? 1 : a.n))};
+}
+// Few zeros (up to 64 MB) go with the sort's launch: a launch less (5 x 9196 positions, V = 10705, h = 48 47 -> 37 us); more are faster on
+// their own.
+constexpr int64_t kFewZeros = 16 << 20;
+bool zeros_ride(const EmbedArgs& a) {
+  return a.ldr == a.h && (int64_t)a.n * a.V * a.h <= kFewZeros && zero_args(a, 4096).all <= 1u << 16;
+}
 hipError_t zeros(const EmbedArgs& a, hipStream_t st) {
   if (a.ldr != a.h) {
     zero_rows_kernel<<<dim3(four_a_block((int64_t)a.n * a.V)), dim3(256), 0, st>>>(a);
     return hipGetLastError();
   }
-  // one piece where nothing lies between the tables, else one per table; fewer than 2^43 bytes: blocks fit 32 bits
-  const bool whole = a.n == 1 || a.lde == (int64_t)a.V * a.h;
-  const int64_t count = (whole ? a.n : 1) * (int64_t)a.V * a.h, blocks = (count + 1023) / 1024, all = blocks * (whole ? 1 : a.n);
-  zeros_kernel<<<dim3((uint32_t)std::min(all, kMostZeros)), dim3(256), 0, st>>>(a.dE, count, a.lde, (uint32_t)blocks, (uint32_t)all);
+  const ZeroArgs z = zero_args(a, 1024);
+  zeros_kernel<<<dim3((uint32_t)std::min<int64_t>(z.all, kMostZeros)), dim3(256), 0, st>>>(z);
   return hipGetLastError();
 }
 
-template <int IPT> hipError_t sort_lds(const EmbedArgs& a, const EmbedGradPlan& p, hipStream_t st) {
+template <int IPT> hipError_t sort_lds(const EmbedArgs& a, const EmbedGradPlan& p, const ZeroArgs& z, hipStream_t st) {
   const size_t lds = (16 * kDigits + 16 + IPT * 1024) * sizeof(uint32_t);
-  sort_lds_kernel<IPT><<<dim3((uint32_t)std::min(a.n, 1 << 16)), dim3(1024), lds, st>>>(a, p);
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sort_lds_kernel<IPT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  const uint32_t sorts = (uint32_t)std::min(a.n, 1 << 16);
+  sort_lds_kernel<IPT><<<dim3(sorts + z.all), dim3(1024), lds, st>>>(a, p, z, sorts);
   return hipGetLastError();
 }
 
@@ -531,21 +561,25 @@ template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const Emb
   char* ws = static_cast<char*>(a.workspace);
   auto words = [&](int64_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
   uint32_t *tok = words(p.tok0), *pos = words(p.pos0);
-  hipError_t e = a.accumulate ? hipSuccess : zeros(a, st);
+  const bool ride = !a.accumulate && zeros_ride(a);
+  const ZeroArgs z = ride ? zero_args(a, 4096) : ZeroArgs{};
+  hipError_t e = a.accumulate || ride ? hipSuccess : zeros(a, st);
   if (e != hipSuccess) return e;
   if (p.lds) {
-    e = a.T <= 1024 ? sort_lds<1>(a, p, st) : a.T <= 2048 ? sort_lds<2>(a, p, st) : sort_lds<4>(a, p, st);
+    e = a.T <= 1024 ? sort_lds<1>(a, p, z, st) : a.T <= 2048 ? sort_lds<2>(a, p, z, st) : a.T <= 4096 ? sort_lds<4>(a, p, z, st) : sort_lds<8>(a, p, z, st);
   } else {
     uint32_t *tok2 = words(p.tok1), *pos2 = words(p.pos1);
     const dim3 grid((uint32_t)std::min((int64_t)a.n * p.tiles, kMostBlocks));
     for (int k = 0; k < p.passes && e == hipSuccess; ++k) {
       const PassArgs q{k ? nullptr : a.tokens, tok, pos, tok2, pos2, words(p.hist), a.n, a.V, a.T, p.tiles, k * p.digit_bits,
                        std::min(p.digit_bits, p.bits - k * p.digit_bits)};
+      const ZeroArgs zk = k ? ZeroArgs{} : z;
+      const dim3 counts(grid.x + zk.all);
       if (tile_of_sort(a.T) == 1024) {
-        count_digits_kernel<1><<<grid, dim3(1024), 0, st>>>(q);
+        count_digits_kernel<1><<<counts, dim3(1024), 0, st>>>(q, zk, grid.x);
         place_keys_kernel<1><<<grid, dim3(1024), 0, st>>>(q);
       } else {
-        count_digits_kernel<4><<<grid, dim3(1024), 0, st>>>(q);
+        count_digits_kernel<4><<<counts, dim3(1024), 0, st>>>(q, zk, grid.x);
         place_keys_kernel<4><<<grid, dim3(1024), 0, st>>>(q);
       }
       e = hipGetLastError();

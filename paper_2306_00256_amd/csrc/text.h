@@ -27,7 +27,7 @@ struct EmbedArgs {
 // How the gradient's positions are brought into the order of their tokens, and its workspace.
 constexpr int kChunk = 16;             // sorted positions that one wavefront adds up
 constexpr int kFewT = 256, kSomeT = 1024;   // positions per agent up to which nothing is sorted: always, with few positions in all
-constexpr int kLdsT = 4096;            // ... up to which one workgroup sorts them in LDS
+constexpr int kLdsT = 8192;            // ... up to which one workgroup sorts them in LDS
 constexpr int64_t kSomePositions = 4096;
 // Positions per workgroup where several sort together: 1024, one a thread, while few workgroups have to add up the others' counts.
 constexpr int tile_of_sort(int64_t T) { return T <= (1 << 16) ? 1024 : 4096; }
