@@ -105,7 +105,7 @@ __device__ __forceinline__ void rank_keys(const uint32_t (&key)[IPT], uint32_t (
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, digits = 1 << bits;
   for (int k = tid; k < 16 * digits; k += 1024) count[k] = 0;
   __syncthreads();
-  uint32_t* mine = count + wave * digits;
+  volatile uint32_t* mine = count + wave * digits;      // (lanes of the wavefront read what others of it wrote)
 #pragma unroll
   for (int j = 0; j < IPT; ++j) {
     const uint32_t d = key[j] >> shift & (digits - 1);
