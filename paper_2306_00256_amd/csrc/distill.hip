@@ -586,8 +586,11 @@ template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& 
   else if constexpr (GRAD) {
     if (packs <= 256 * 4) distill_row_kernel<T, 256, 4, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
     else if (packs <= 256 * 8) distill_row_kernel<T, 256, 8, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
+    else if (packs <= 256 * 12) distill_row_kernel<T, 256, 12, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
     else if (packs <= 256 * 16) distill_row_kernel<T, 256, 16, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
+    else if (packs <= 512 * 12) distill_row_kernel<T, 512, 12, TWO, true, false><<<blocks, dim3(512), 0, st>>>(a, rows);
     else if (packs <= 512 * 16) distill_row_kernel<T, 512, 16, TWO, true, false><<<blocks, dim3(512), 0, st>>>(a, rows);
+    else if (packs <= 1024 * 12) distill_row_kernel<T, 1024, 12, TWO, true, true><<<dim3((uint32_t)std::min<int64_t>(rows, 256)), dim3(1024), 0, st>>>(a, rows);
     else distill_row_kernel<T, 1024, 16, TWO, true, true><<<dim3((uint32_t)std::min<int64_t>(rows, 256)), dim3(1024), 0, st>>>(a, rows);
   }
   return hipGetLastError();
