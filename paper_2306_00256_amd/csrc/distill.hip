@@ -220,6 +220,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
   uint32_t mine = tid * 16;
   auto at = [&](int j) { return mine + (uint32_t)(j * THREADS * 16); };
   auto there = [&](int j) { return at(j) < bytes; };
+  auto some_there = [&](int j) { return (uint32_t)(j * THREADS * 16) < bytes; };      // of the workgroup's
   auto pack_of = [&](int j, const T* s, uint32_t limit) {
     return P::load_stream(reinterpret_cast<const T*>(reinterpret_cast<const char*>(s) + min(at(j), limit)));
   };
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       x[j].again();
-      st.template add<P, VEC>(x[j], there(j), k, true);
+      if (some_there(j)) st.template add<P, VEC>(x[j], there(j), k, true);
       __builtin_amdgcn_sched_barrier(0);
     }
     bool run = true;
@@ -358,7 +359,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
           }
           if (LOOP && j >= kLag) {
             x[j - kLag].again();
-            st1.template add<P, VEC>(x[j - kLag], there(j - kLag), k);
+            if (some_there(j - kLag)) st1.template add<P, VEC>(x[j - kLag], there(j - kLag), k);
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -578,7 +579,7 @@ template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& 
     return hipGetLastError();
   }
   // As many threads as the row needs with 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
-  // unit, of which some load while others compute: one row each (7936 rows of 32000 bf16, two softmaxes 206 us; looping, with the
+  // unit, of which some load while others compute: one row each (7936 rows of 32000 bf16, two softmaxes 201 us; looping, with the
   // next row's loads in between, 242).  Rows of 1024 threads have the compute unit to themselves and loop (15872 rows of
   // 128000 bf16 1507 us, 5.1 TB/s; with the loads between the rows it took 230 us more).
   if (packs <= 64) distill_row_kernel<T, 64, 1, TWO, GRAD, false><<<blocks, dim3(64), 0, st>>>(a, rows);
