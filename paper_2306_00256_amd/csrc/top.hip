@@ -363,7 +363,7 @@ template <typename T> hipError_t launch(const TopArgs& a, hipStream_t st) {
   // 256 threads with up to 16 packs each: several rows on a compute unit, of which some load while others look for their threshold
   // (7936 rows of 32000 bf16, K = 64: 120 us; 512 threads with 8 packs 140, 128 with 32 212, 1024 with 4 376).  Longer rows
   // in parts: 1000 rows of 33216 fp32, K = 157, 67 us, in one tile of 512 threads 89.  Many short rows by a wavefront each, which
-  // needs no barriers (87219 rows of 2304 bf16, K = 6: 218 us, by 256 threads 313); few of them are done sooner by more threads.
+  // needs no barriers (87219 rows of 2304 bf16, K = 6: 143 us, by 256 threads 313); few of them are done sooner by more threads.
   const dim3 grid((uint32_t)std::min((int64_t)a.rows * plan.parts, kMostTopBlocks));
   if (packs <= 64) top_kernel<T, 64, 1><<<grid, dim3(64), 0, st>>>(a, plan);
   else if (packs <= 64 * 4) top_kernel<T, 64, 4><<<grid, dim3(64), 0, st>>>(a, plan);
