@@ -578,7 +578,7 @@ template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& 
     stream<T, TWO>(t, st);
     return hipGetLastError();
   }
-  // As many threads as the row needs with 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
+  // As many threads as the row needs with 12 or 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
   // unit, of which some load while others compute: one row each (7936 rows of 32000 bf16, two softmaxes 201 us; looping, with the
   // next row's loads in between, 242).  Rows of 1024 threads have the compute unit to themselves and loop (15872 rows of
   // 128000 bf16 1507 us, 5.1 TB/s; with the loads between the rows it took 230 us more).
