@@ -398,8 +398,9 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
 
 // ---- rows that stream through ----
 // Longer rows than registers hold: a workgroup reads the row twice, the second time mostly from the last-level cache.  The loss alone
-// needs a row once and no registers to keep it in: more workgroups, more loads in flight (975 rows of 50021 fp16 28.4 us,
-// from a register tile 32.8; four packs a thread at once: with more, or as a ring, the registers cost more than it gains).  Few rows:
+// needs a row once and no registers to keep it in: more workgroups, more loads in flight (975 rows of 50021 fp16 25.2 us,
+// from a register tile 32.8; four packs a thread at once: with more, or as a ring, the registers cost more than it gains; GRAD: without
+// a gradient the kernel has neither its registers nor its table, 46 to 51 registers in place of 60 to 80: 28.5 us with them).  Few rows:
 // `parts` workgroups take a row's columns; one launch leaves each part's maximum and sums in the workspace (and the logits at the
 // entries' places, which the gradient may overwrite), a second one joins them and does the rest.
 enum StreamMode : int { STREAM_ALL = 0, STREAM_STATS = 1, STREAM_REST = 2 };
@@ -411,12 +412,12 @@ struct StreamArgs {
   float* values;       // K + 1 per row
 };
 
-template <typename T, int THREADS, bool TWO>
-__global__ __launch_bounds__(THREADS) void distill_stream_kernel(StreamArgs t) {
+template <typename T, int THREADS, bool TWO, bool GRAD>
+__global__ __launch_bounds__(THREADS, GRAD ? 6 : 8) void distill_stream_kernel(StreamArgs t) {
   constexpr int VEC = kVec<T>, WAVES = THREADS / 64, AHEAD = 4;
   using P = Pack<T, VEC>;
   __shared__ float red[6][16];
-  __shared__ EntryTable table;
+  __shared__ EntryTable table;                                // (none without uses)
   const DistillArgs& a = t.a;
   const int tid = threadIdx.x;
   const Scales<TWO> k(a);
@@ -426,16 +427,16 @@ __global__ __launch_bounds__(THREADS) void distill_stream_kernel(StreamArgs t) {
     const int32_t part = (int32_t)(unit - row * t.parts), c0 = part * t.cols, c1 = min(c0 + t.cols, a.V);
     const int32_t packed = c0 + (c1 - c0) / VEC * VEC;       // the rest, fewer than a pack, one by one
     const T* s = static_cast<const T*>(a.logits) + row * a.ld;
-    T* grad = a.grad ? static_cast<T*>(a.grad) + row * a.ldg : nullptr;
+    T* grad = GRAD ? static_cast<T*>(a.grad) + row * a.ldg : nullptr;
     Entries<1> own;
     own.load<THREADS>(a, row);
     own.settle(a);
     __syncthreads();                                          // (shared arrays of the unit before)
-    if (grad && t.mode != STREAM_STATS) table.clear<THREADS>();
+    if (GRAD) table.clear<THREADS>();
     if (own.w == 0.0f) {
       if (t.mode != STREAM_STATS) {
         if (a.loss && tid == 0 && part == 0) a.loss[row] = 0.0f;
-        if (grad) {
+        if (GRAD) {
           Pack<T, VEC> z;
           z.v = 0;
           for (int32_t c = c0 + tid * VEC; c < packed; c += THREADS * VEC) z.store_stream(grad + c);
@@ -514,11 +515,11 @@ __global__ __launch_bounds__(THREADS) void distill_stream_kernel(StreamArgs t) {
     int slot = 0;
     if (own.id[0] >= 0) {
       term = entry_term(p, (own.u[0] - um) * inv_tau - logf(usum), logf(q), se - m, inv_tau);
-      if (grad && f.cs != 0.0f) slot = table.put(own.id[0], p);
+      if (GRAD && f.cs != 0.0f) slot = table.put(own.id[0], p);
     }
     term = wave_all(term, Add());
     if (tid % 64 == 0) red[5][tid / 64] = term;
-    if (grad) {
+    if (GRAD) {
       for (int32_t c = c0 + tid * VEC; c < packed; c += THREADS * VEC * AHEAD) {
         Pack<T, VEC> x[AHEAD];
 #pragma unroll
@@ -543,7 +544,7 @@ __global__ __launch_bounds__(THREADS) void distill_stream_kernel(StreamArgs t) {
       if (f.ch != 0.0f) loss += f.ch * (logf(r) - (sl - m));
       a.loss[row] = loss;
     }
-    if (grad && !f.zero) {
+    if (GRAD && !f.zero) {
       if (f.cs != 0.0f && own.id[0] >= c0 && own.id[0] < c1)
         grad[own.id[0]] = from_float<T>(gradient_there<TWO>(se - m, table.sum(slot) + (usum - usum), own.id[0] == own.label, k, f, q, r));
       if (f.ch != 0.0f && tid == THREADS - 1 && own.label >= c0 && own.label < c1 && !table.has(own.label))
@@ -554,10 +555,10 @@ __global__ __launch_bounds__(THREADS) void distill_stream_kernel(StreamArgs t) {
 
 constexpr int64_t kMostRowBlocks = 1 << 21;       // (a launch has fewer than 2^32 threads)
 
-template <typename T, bool TWO> void stream(const StreamArgs& t, hipStream_t st) {
+template <typename T, bool TWO, bool GRAD> void stream(const StreamArgs& t, hipStream_t st) {
   const dim3 grid((uint32_t)std::min(t.rows * t.parts, kMostRowBlocks));
-  if (t.cols <= 256 * kVec<T> * 8) distill_stream_kernel<T, 256, TWO><<<grid, dim3(256), 0, st>>>(t);
-  else distill_stream_kernel<T, 512, TWO><<<grid, dim3(512), 0, st>>>(t);
+  if (t.cols <= 256 * kVec<T> * 8) distill_stream_kernel<T, 256, TWO, GRAD><<<grid, dim3(256), 0, st>>>(t);
+  else distill_stream_kernel<T, 512, TWO, GRAD><<<grid, dim3(512), 0, st>>>(t);
 }
 
 template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& a, hipStream_t st) {
@@ -572,10 +573,10 @@ template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& 
       t.stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.stats);
       t.values = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.values);
       t.mode = STREAM_STATS;
-      stream<T, TWO>(t, st);
+      stream<T, TWO, false>(t, st);
       t.mode = STREAM_REST;
     }
-    stream<T, TWO>(t, st);
+    stream<T, TWO, GRAD>(t, st);
     return hipGetLastError();
   }
   // As many threads as the row needs with 12 or 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
