@@ -55,31 +55,59 @@ template <int EPT> struct Entries {
   }
 };
 
-// A row's entries by their places, in LDS: open addressing in twice as many slots as there are entries at most, and each place's shares
-// summed as whole numbers of 2^-62, whose order does not matter -- an id that comes twice takes both.
+// A row's entries by their places, in LDS: open addressing in twice as many slots as there are entries at most.  Every entry keeps its
+// share as the fp32 number it is.  Where entries share a place, the shares are summed as whole numbers, whose order does not matter,
+// of 2^-46 of the power of two at or below the place's largest share: a unit of the row's own would leave small shares no bits.
 constexpr int kSlots = 2 * kTopMax;
-struct EntryTable {
+struct alignas(16) EntryTable {
   int32_t id[kSlots];          // -1: empty
-  unsigned long long p[kSlots];
-  template <int THREADS> __device__ __forceinline__ void clear() {
-    for (int k = threadIdx.x; k < kSlots; k += THREADS) {
-      id[k] = -1;
-      p[k] = 0;
-    }
+  unsigned long long cell[kSlots];             // (exponent of the largest share) 2^56 + sum, where some entries share a place
+  int32_t at[kTopMax];         // an entry's place, -1: none
+  float p[kTopMax];            // its share, then all of its place's
+  int32_t twice;               // whether entries share places
+  template <int THREADS, int EPT> __device__ __forceinline__ void begin(const Entries<EPT>& own) {
+    typedef int32_t I4 __attribute__((ext_vector_type(4)));
+    for (int k = threadIdx.x; k < kSlots / 4; k += THREADS) reinterpret_cast<I4*>(id)[k] = I4{-1, -1, -1, -1};
+#pragma unroll
+    for (int e = 0; e < EPT; ++e)
+      if (THREADS <= kTopMax || threadIdx.x < kTopMax) at[e * THREADS + threadIdx.x] = own.id[e];
+    if (threadIdx.x == 0) twice = 0;
   }
   __device__ static __forceinline__ uint32_t first(int32_t v) { return ((uint32_t)v * 0x9e3779b1u) >> 23; }       // of 512
-  // the slot of v, taken if there is none yet (v >= 0; K <= 256 of 512 are taken, so the search ends)
-  __device__ __forceinline__ int put(int32_t v, float share) {
+  // entry e's share at its place v (v >= 0; K <= 256 of 512 slots are taken, so the search ends)
+  __device__ __forceinline__ void put(int e, int32_t v, float share) {
+    p[e] = share;
     uint32_t k = first(v);
     for (;;) {
       const int32_t was = atomicCAS(&id[k], -1, v);
+      if (was == v) twice = 1;
       if (was == -1 || was == v) break;
       k = (k + 1) % kSlots;
     }
-    atomicAdd(&p[k], (unsigned long long)(fmaxf(share, 0.0f) * 0x1p62f));       // (NaN: then the row's sum of exponentials is)
-    return (int)k;
   }
-  __device__ __forceinline__ float sum(int k) const { return (float)p[k] * 0x1p-62f; }
+  // p[e]: what entry e's place got, for the thread that put it (behind a barrier, by all threads)
+  template <int THREADS> __device__ __forceinline__ void join(int K) {
+    if (!twice) return;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));              // (addresses worked out here: few rows come this way)
+#pragma unroll 1
+    for (int k = tid; k < kSlots; k += THREADS) cell[k] = 0;
+    __syncthreads();
+    auto cell_of = [&](int32_t v) {
+      uint32_t k = first(v);
+      while (id[k] != v) k = (k + 1) % kSlots;
+      return &cell[k];
+    };
+    auto each = [&](auto&& f) {
+#pragma unroll 1
+      for (int e = tid; e < K; e += THREADS)
+        if (at[e] >= 0) f(p[e], cell_of(at[e]));
+      __syncthreads();
+    };
+    each([&](float x, unsigned long long* c) { atomicMax(c, (unsigned long long)(__float_as_uint(x) >> 23 & 255) << 56); });
+    each([&](float x, unsigned long long* c) { atomicAdd(c, (unsigned long long)__builtin_amdgcn_ldexpf(x == x ? x : 0.0f, 127 + 46 - (int)(*c >> 56))); });
+    each([&](float& x, unsigned long long* c) { x = x == x ? __builtin_amdgcn_ldexpf((float)(*c & (1ull << 56) - 1), (int)(*c >> 56) - 127 - 46) : x; });
+  }
   __device__ __forceinline__ bool has(int32_t v) const {
     for (uint32_t k = first(v); id[k] != -1; k = (k + 1) % kSlots)
       if (id[k] == v) return true;
@@ -203,7 +231,7 @@ template <bool TWO> struct Running {
 // registers that become free and their statistics taken kLag packs later, so that memory is busy all the time.
 constexpr int kLag = 4;
 template <typename T, int THREADS, int NP, bool TWO, bool GRAD, bool LOOP>
-__global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void distill_row_kernel(DistillArgs a, int64_t rows) {
+__global__ __launch_bounds__(THREADS, NP == 1 ? 5 : THREADS < 1024 && NP == 16 ? 4 : 1) void distill_row_kernel(DistillArgs a, int64_t rows) {
   constexpr int VEC = kVec<T>, WAVES = THREADS / 64, EPT = THREADS >= kTopMax ? 1 : kTopMax / THREADS;
   using P = Pack<T, VEC>;
   constexpr int SETS = LOOP ? 2 : 1;                       // in turn: a row's are read behind its barriers
@@ -289,7 +317,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
       sl = to_float(s[max(own.label, 0)]);
       if (more) next.template load<THREADS>(a, row1);
 
-      if (GRAD) table[set].template clear<THREADS>();
+      if (GRAD) table[set].template begin<THREADS>(own);
 
       float um = kLowest, usum = 0.0f, ue[EPT];
 #pragma unroll
@@ -324,7 +352,6 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
       }
 
       float term = 0.0f;
-      int slot[EPT];
       const float lq = logf(q), lu = logf(usum);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) {
@@ -332,7 +359,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
           ue[e] = exp2_fast((own.u[e] - um) * (inv_tau * kLog2e));
           const float p = ue[e] / usum;
           term += entry_term(p, (own.u[e] - um) * inv_tau - lu, lq, se[e] - m, inv_tau);
-          if (GRAD && f.cs != 0.0f) slot[e] = table[set].put(own.id[e], p);
+          if (GRAD && f.cs != 0.0f) table[set].put(e * THREADS + tid, own.id[e], p);
         }
       }
       term = wave_all(term, Add());
@@ -380,10 +407,11 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 && NP == 16 ? 4 : 1) void d
       // the places of the entries and of the label once more, whole: an id that comes twice takes both shares
       if (GRAD) {
         T* grad = grad_of(row);
+        if (f.cs != 0.0f) table[set].template join<THREADS>(a.K);
 #pragma unroll
         for (int e = 0; e < EPT; ++e)
           if (f.cs != 0.0f && own.id[e] >= 0)
-            grad[own.id[e]] = from_float<T>(gradient_there<TWO>(se[e] - m, table[set].sum(slot[e]) + (usum - usum), own.id[e] == own.label, k, f, q, r));
+            grad[own.id[e]] = from_float<T>(gradient_there<TWO>(se[e] - m, table[set].p[e * THREADS + tid], own.id[e] == own.label, k, f, q, r));
         if (f.ch != 0.0f && tid == THREADS - 1 && !table[set].has(own.label))
           grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
       }
@@ -432,7 +460,7 @@ __global__ __launch_bounds__(THREADS, GRAD ? 6 : 8) void distill_stream_kernel(S
     own.load<THREADS>(a, row);
     own.settle(a);
     __syncthreads();                                          // (shared arrays of the unit before)
-    if (GRAD) table.clear<THREADS>();
+    if (GRAD) table.template begin<THREADS>(own);
     if (own.w == 0.0f) {
       if (t.mode != STREAM_STATS) {
         if (a.loss && tid == 0 && part == 0) a.loss[row] = 0.0f;
@@ -512,10 +540,9 @@ __global__ __launch_bounds__(THREADS, GRAD ? 6 : 8) void distill_stream_kernel(S
     const Factors f(a, own.w, usum != 0.0f, own.label >= 0, q, r);
     const float p = own.id[0] >= 0 ? ue / usum : 0.0f;
     float term = 0.0f;
-    int slot = 0;
     if (own.id[0] >= 0) {
       term = entry_term(p, (own.u[0] - um) * inv_tau - logf(usum), logf(q), se - m, inv_tau);
-      if (GRAD && f.cs != 0.0f) slot = table.put(own.id[0], p);
+      if (GRAD && f.cs != 0.0f) table.put(tid, own.id[0], p);
     }
     term = wave_all(term, Add());
     if (tid % 64 == 0) red[5][tid / 64] = term;
@@ -545,8 +572,9 @@ __global__ __launch_bounds__(THREADS, GRAD ? 6 : 8) void distill_stream_kernel(S
       a.loss[row] = loss;
     }
     if (GRAD && !f.zero) {
+      if (f.cs != 0.0f) table.template join<THREADS>(a.K);
       if (f.cs != 0.0f && own.id[0] >= c0 && own.id[0] < c1)
-        grad[own.id[0]] = from_float<T>(gradient_there<TWO>(se - m, table.sum(slot) + (usum - usum), own.id[0] == own.label, k, f, q, r));
+        grad[own.id[0]] = from_float<T>(gradient_there<TWO>(se - m, table.p[tid], own.id[0] == own.label, k, f, q, r));
       if (f.ch != 0.0f && tid == THREADS - 1 && own.label >= c0 && own.label < c1 && !table.has(own.label))
         grad[own.label] = from_float<T>(gradient_there<TWO>(sl - m, 0.0f, true, k, f, q, r));
     }
