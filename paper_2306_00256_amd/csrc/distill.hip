@@ -150,9 +150,11 @@ template <typename T, bool TWO> __device__ __forceinline__ float gradient_at(flo
   return f.both * exp2_fast(x * k.kq);
 }
 
-// One entry's part of the loss before its factors: p (log p - log q_id) with x = s_id - m.
-__device__ __forceinline__ float entry_term(float p, float logp, float logq_sum, float x, float inv_tau) {
-  return p != 0.0f ? p * (logp + logq_sum - x * inv_tau) : 0.0f;
+// One entry's part of the loss before its factors: tau p (log p - log q_id), with du and x the differences of its value and its logit from
+// the largest, and lu, lq the logarithms of the sums.  (Times tau: x / tau alone may pass what fp32 holds where tau < 1 and the
+// logit is the lowest finite one.)
+__device__ __forceinline__ float entry_term(float p, float du, float lu, float lq, float x, float tau) {
+  return p != 0.0f ? p * (du - x + tau * (lq - lu)) : 0.0f;
 }
 
 // The gradient at an entry's place or at the label, all of it.
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(THREADS, NP == 1 ? 5 : THREADS < 1024 && NP == 16 ?
         if (own.id[e] >= 0) {
           ue[e] = exp2_fast((own.u[e] - um) * (inv_tau * kLog2e));
           const float p = ue[e] / usum;
-          term += entry_term(p, (own.u[e] - um) * inv_tau - lu, lq, se[e] - m, inv_tau);
+          term += entry_term(p, own.u[e] - um, lu, lq, se[e] - m, a.tau);
           if (GRAD && f.cs != 0.0f) table[set].put(e * THREADS + tid, own.id[e], p);
         }
       }
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(THREADS, NP == 1 ? 5 : THREADS < 1024 && NP == 16 ?
       if (a.loss && tid == 0) {
         float sum = 0.0f, loss = 0.0f;
         for (int w = 0; w < WAVES; ++w) sum += red[set][5][w];
-        if (f.cs != 0.0f) loss += f.cs * a.tau * a.tau * sum;
+        if (f.cs != 0.0f) loss += f.cs * a.tau * sum;
         if (f.ch != 0.0f) loss += f.ch * (logf(r) - (sl - m));
         a.loss[row] = loss;
       }
@@ -541,7 +543,7 @@ __global__ __launch_bounds__(THREADS, GRAD ? 6 : 8) void distill_stream_kernel(S
     const float p = own.id[0] >= 0 ? ue / usum : 0.0f;
     float term = 0.0f;
     if (own.id[0] >= 0) {
-      term = entry_term(p, (own.u[0] - um) * inv_tau - logf(usum), logf(q), se - m, inv_tau);
+      term = entry_term(p, own.u[0] - um, logf(usum), logf(q), se - m, a.tau);
       if (GRAD && f.cs != 0.0f) table.put(tid, own.id[0], p);
     }
     term = wave_all(term, Add());
@@ -567,7 +569,7 @@ __global__ __launch_bounds__(THREADS, GRAD ? 6 : 8) void distill_stream_kernel(S
       float loss = 0.0f;
       float sum = 0.0f;
       for (int w = 0; w < WAVES; ++w) sum += red[5][w];
-      if (f.cs != 0.0f) loss += f.cs * a.tau * a.tau * sum;
+      if (f.cs != 0.0f) loss += f.cs * a.tau * sum;
       if (f.ch != 0.0f) loss += f.ch * (logf(r) - (sl - m));
       a.loss[row] = loss;
     }

@@ -1,4 +1,4 @@
-"""GPU parity: a teacher's small shares in the distillation's gradient.
+"""GPU parity: a teacher's small shares and a student's lowest logits in the distillation's loss and gradient.
 
 Tolerances.  A share is exp(x) / sum with x = (u - largest) / temperature: the argument takes four roundings at most (difference,
 1 / temperature, its product with log2 e, the product), which the exponential turns into 4 |x| half fp32 steps of the share; the
@@ -86,6 +86,26 @@ def test_places_that_many_entries_name(env):
     top[[first, first + 1]] = top[[first + 1, first]]
     _, again = _call(env, torch.from_numpy(x).cuda().repeat(2, 1), top, ids, 1.0)
     assert torch.equal(again, grad)
+
+
+@pytest.mark.parametrize("dtype,R,V", SIZES[:6])
+def test_lowest_logits_at_entries_below_temperature_one(env, dtype, R, V):
+    """The type's lowest finite value is an ordinary logit: at temperature 0.5 an entry's loss there, 0.25 p * 6.8e38, is a number of
+    fp32 (and a large one: all other terms together are below half a step of it).  Its error is that of p and of some products:
+    64 half steps."""
+    torch, _ = env
+    lowest = float(torch.finfo(getattr(torch, dtype)).min)
+    ids, top = np.array([3, 9, 30], dtype=np.int32), np.array([2.0, 1.25, 0.5], dtype=np.float32)
+    x = np.random.default_rng(V).uniform(-2, 2, V).astype(np.float32)
+    x[9] = lowest
+    row = torch.from_numpy(x).to(getattr(torch, dtype))
+    want, want_grad, _ = OT.distill_row(row.double().numpy(), top, ids, 0.5, 0.0, None, 1.0)
+    assert 1e36 < want < 1e38
+    for grad in (True, False):
+        loss, _ = _call(env, row.cuda().repeat(R, 1), top, ids, 0.5, grad=grad)
+        assert (np.abs(loss.double().cpu().numpy() - want) <= 64 * 2.0 ** -24 * want).all()
+    _, g = _call(env, row.cuda().repeat(R, 1), top, ids, 0.5)
+    assert (np.abs(g[:, 9].double().cpu().numpy() - want_grad[9]) <= (64 * 2.0 ** -24 + HALF_STEP[dtype]) * abs(want_grad[9]) * 1.01).all()
 
 
 @pytest.mark.parametrize("dtype,R,V", SIZES)
