@@ -353,7 +353,9 @@ int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t*
  *   loss = weight [ (1 - hard) temperature^2 sum_k p_k (log p_k - log q_id_k)  +  hard (-log r_label) ]
  *   gradient by s_v = weight [ (1 - hard) temperature (q_v - sum_{k: id_k = v} p_k)  +  hard (r_v - [v = label]) ]
  * The teacher's row is the position's own or, with `peer`, position t of agent peer[i] (ceca_schedule's map, say): agents
- * that teach each other read each other's entries in place.
+ * that teach each other read each other's entries in place.  A teacher's distribution means something for the input it was
+ * computed from: with `peer`, position t has to hold the same input for every agent (the same tokens up to t, a shared batch),
+ * which this call cannot see.
  *   - An id outside [0, V) or a value of -inf is no entry.  An id that comes twice counts twice.
  *   - A row without entries has no soft term, one whose label is outside [0, V) no hard term; K = 0 with labels and hard > 0
  *     is the plain cross entropy.
