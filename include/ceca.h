@@ -363,6 +363,9 @@ int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t*
  *     The type's lowest finite value is an ordinary logit.
  *   - A row with neither term, or with every logit -inf, has loss 0 and a zero gradient.  So has one of weight 0, whose logits
  *     and entries are not looked at (padding may hold anything).
+ *   - Exponentials are taken of differences from the row's largest value: with x such a difference over the temperature, a share is
+ *     off by up to (4 |x| + V / 64 + 64) 2^-24 of itself, and one below 2^-126 of the largest is zero (an entry so small has no part in loss
+ *     and gradient, masked or not).
  *   - Otherwise a NaN or +inf among a row's logits makes its loss and its whole gradient NaN; one among its entries' values its soft
  *     loss and the gradient at its entries' places. */
 #define CECA_TOP_MAX 256
