@@ -97,6 +97,22 @@ int32_t ceca_last_window_on_one_xcd(void);
 int32_t ceca_describe_step_launch(int32_t n, int64_t d, int64_t ld, int32_t r, int32_t port, int32_t kind,
                                   int32_t in_place, int32_t* out);
 
+/* The kernels that a call of a language-model operator launches, so that a test that means one of them can ask whether its
+ * sizes reach it.  Nothing is launched.  n agents with T positions each; type: of the activations or logits; out: host, 5 int32
+ * (0 where not named below):
+ *   CECA_TEXT_EMBED    ceca_embed, width = h: columns per lane, positions per wavefront
+ *   CECA_TEXT_GRAD     ceca_embed_grad, width = h: columns per lane; tokens per lane where nothing is sorted; positions per thread where one
+ *                      workgroup sorts an agent's; positions per workgroup where several do; who writes the zeros (1 the sort's launch,
+ *                      2 a launch over whole pieces, 3 one over rows)
+ *   CECA_TEXT_DISTILL  ceca_distill, width = K: threads per workgroup, packs of 16 bytes per thread (0: rows stream), whether workgroups loop
+ *                      over rows, parts of a row
+ *   CECA_TEXT_TOP      ceca_top_logits with n T rows, width = K: threads per workgroup, packs per thread, parts of a row, merging launches
+ * flags: CECA_TEXT_ACCUMULATE, CECA_TEXT_APART (something lies between the agents' tables), CECA_TEXT_PITCH (and between the rows of a
+ * table), CECA_TEXT_WITH_GRAD (ceca_distill with a gradient). */
+enum { CECA_TEXT_EMBED = 0, CECA_TEXT_GRAD = 1, CECA_TEXT_DISTILL = 2, CECA_TEXT_TOP = 3 };
+enum { CECA_TEXT_ACCUMULATE = 1, CECA_TEXT_APART = 2, CECA_TEXT_PITCH = 4, CECA_TEXT_WITH_GRAD = 8 };
+int32_t ceca_describe_text_launch(int32_t call, int32_t type, int32_t n, int32_t T, int32_t V, int32_t width, int32_t flags, int32_t* out);
+
 /* An elementwise kernel with `reads` streaming reads (1..3: a, then b, then c) and `writes` streaming
  * writes (1..2: o1, then o2) per element, so that a benchmark can report, from the same run, the bandwidth
  * the device gives the simplest kernel with a step's traffic mix: 3 reads + 2 writes for a full round of

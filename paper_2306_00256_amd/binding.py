@@ -17,6 +17,8 @@ TOPO_RING, TOPO_STATIC_EXP, TOPO_ONE_PEER_EXP = 0, 1, 2
 MIX_MAX = 16
 TOP_MAX = 256
 TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2            # CECA_F32, CECA_BF16, CECA_F16
+TEXT_EMBED, TEXT_GRAD, TEXT_DISTILL, TEXT_TOP = range(4)
+TEXT_ACCUMULATE, TEXT_APART, TEXT_PITCH, TEXT_WITH_GRAD = 1, 2, 4, 8
 # forms of the minibatch calls, as ceca_last_form (ceca_test.h) names them
 FORM_NONE, FORM_STEP_SINGLE, FORM_STEP_ONE_PASS, FORM_STEP_TWO_PASS, FORM_RUN_WINDOW, FORM_RUN_HALF_STEPS, FORM_RUN_MESSAGES, FORM_RUN_TWO_PASS, FORM_RUN_STEPS = range(9)
 
@@ -27,7 +29,7 @@ EXPORTS = (
     "ceca_last_error", "ceca_last_hip_error",
 )
 # include/ceca_test.h: launch-shape overrides and probe kernels for tests and measurement, not the product ABI
-TEST_EXPORTS = ("ceca_set_option", "ceca_reset_options", "ceca_stream_probe", "ceca_describe_step_launch", "ceca_last_form", "ceca_last_window_on_one_xcd")
+TEST_EXPORTS = ("ceca_set_option", "ceca_reset_options", "ceca_stream_probe", "ceca_describe_step_launch", "ceca_describe_text_launch", "ceca_last_form", "ceca_last_window_on_one_xcd")
 
 
 class CecaError(RuntimeError):
@@ -141,6 +143,8 @@ def lib():
         L.ceca_describe_step_launch.argtypes = [C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                                 C.POINTER(C.c_int32)]
         L.ceca_describe_step_launch.restype = C.c_int32
+        L.ceca_describe_text_launch.argtypes = [C.c_int32] * 7 + [C.c_void_p]
+        L.ceca_describe_text_launch.restype = C.c_int32
         L.ceca_last_form.argtypes = []
         L.ceca_last_form.restype = C.c_int32
         L.ceca_last_window_on_one_xcd.argtypes = []
@@ -468,6 +472,13 @@ def ceca_describe_step_launch(n: int, d: int, ld: int, r: int, port: int, kind: 
     out = (C.c_int32 * 6)()
     _check(lib().ceca_describe_step_launch(n, d, ld, r, port, int(kind), int(in_place), out))
     return dict(zip(("rows", "band", "wg_per_cu", "stretch", "stretches_per_cycle", "vec"), list(out)))
+
+
+def ceca_describe_text_launch(call: int, type: int, n: int, T: int, V: int, width: int, flags: int = 0) -> tuple:
+    """The kernels that a language-model operator's call of these sizes launches (ceca_test.h says what the five numbers are)."""
+    out = (C.c_int32 * 5)()
+    _check(lib().ceca_describe_text_launch(call, type, n, T, V, width, flags, out))
+    return tuple(out)
 
 
 def ceca_last_form() -> int:

@@ -1507,6 +1507,32 @@ int32_t ceca_top_logits(const void* logits, int32_t type, int64_t ld, int32_t ro
   return e == hipSuccess ? CECA_OK : hip_fail(e, "top logits kernel launch");
 }
 
+int32_t ceca_describe_text_launch(int32_t call, int32_t type, int32_t n, int32_t T, int32_t V, int32_t width, int32_t flags, int32_t* out) {
+  if (!out) return fail(CECA_EINVAL, "null pointer");
+  if (call < CECA_TEXT_EMBED || call > CECA_TEXT_TOP || flags < 0 || flags > 15) return fail(CECA_EINVAL, "unknown call %d or flags %d", call, flags);
+  for (int k = 0; k < 5; ++k) out[k] = 0;
+  if (call <= CECA_TEXT_GRAD) {
+    // stand-in addresses (never dereferenced), far apart
+    void* const at[] = {reinterpret_cast<void*>(uintptr_t(1) << 50), reinterpret_cast<void*>(uintptr_t(1) << 52), reinterpret_cast<void*>(uintptr_t(1) << 54)};
+    ceca::EmbedArgs a{};
+    a.n = n;  a.V = V;  a.h = width;  a.T = T;  a.type = type;  a.accumulate = flags & CECA_TEXT_ACCUMULATE;
+    a.ldr = (int64_t)width + (flags & CECA_TEXT_PITCH ? 1 : 0);
+    a.lde = (int64_t)V * a.ldr + (flags & CECA_TEXT_APART ? 1 : 0);
+    int64_t tb, rb;
+    const int32_t rc = check_tables(at[0], a.lde, a.ldr, n, V, width, at[1], type, width, at[2], T, &tb, &rb);
+    if (rc != CECA_OK) return rc;
+    if (call == CECA_TEXT_EMBED) ceca::describe_embed(a, out);
+    else ceca::describe_embed_grad(a, out);
+    return CECA_OK;
+  }
+  if (n < 1 || T < 0 || (int64_t)n * T > INT32_MAX) return fail(CECA_EINVAL, "need n >= 1, T >= 0 and n T < 2^31 (n = %d, T = %d)", n, T);
+  const int32_t rc = check_top(type, n * T, V, std::max(width, call == CECA_TEXT_DISTILL ? 1 : width));
+  if (rc != CECA_OK) return rc;
+  if (call == CECA_TEXT_DISTILL) ceca::describe_distill((int64_t)n * T, V, width, type, flags & CECA_TEXT_WITH_GRAD, out);
+  else ceca::describe_top((int64_t)n * T, V, width, type, out);
+  return CECA_OK;
+}
+
 int32_t ceca_describe_step_launch(int32_t n, int64_t d, int64_t ld, int32_t r, int32_t port, int32_t kind,
                                   int32_t in_place, int32_t* out) {
   if (!out) return fail(CECA_EINVAL, "null pointer");

@@ -585,45 +585,59 @@ __global__ __launch_bounds__(THREADS, GRAD ? 6 : 8) void distill_stream_kernel(S
 
 constexpr int64_t kMostRowBlocks = 1 << 21;       // (a launch has fewer than 2^32 threads)
 
-template <typename T, bool TWO, bool GRAD> void stream(const StreamArgs& t, hipStream_t st) {
+// A workgroup's threads, and the packs of a row that each holds (0: the row streams).
+struct DistillTile {
+  int32_t threads, packs;
+  bool loop;
+};
+// As many threads as the row needs with 12 or 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
+// unit, of which some load while others compute: one row each (7936 rows of 32000 bf16, two softmaxes 201 us; looping, with the
+// next row's loads in between, 242).  Rows of 1024 threads have the compute unit to themselves and loop (15872 rows of
+// 128000 bf16 1507 us, 5.1 TB/s; with the loads between the rows it took 230 us more).
+DistillTile tile_of(const DistillPlan& plan, int32_t V, int type, bool grad) {
+  const int32_t vec = type == TYPE_F32 ? 4 : 8, packs = V / vec;
+  // (the loss alone streams rows of more than 256 packs)
+  if (plan.parts > 1 || packs > 1024 * 16 || (!grad && packs > 256)) return {plan.cols <= 256 * vec * 8 ? 256 : 512, 0, false};
+  for (const DistillTile t : {DistillTile{64, 1, false}, {64, 4, false}, {256, 4, false}, {256, 8, false}, {256, 12, false}, {256, 16, false}, {512, 12, false}, {512, 16, false}, {1024, 12, true}})
+    if (packs <= t.threads * t.packs) return t;
+  return {1024, 16, true};
+}
+
+template <typename T, bool TWO, bool GRAD> void stream(const StreamArgs& t, int32_t threads, hipStream_t st) {
   const dim3 grid((uint32_t)std::min(t.rows * t.parts, kMostRowBlocks));
-  if (t.cols <= 256 * kVec<T> * 8) distill_stream_kernel<T, 256, TWO, GRAD><<<grid, dim3(256), 0, st>>>(t);
+  if (threads == 256) distill_stream_kernel<T, 256, TWO, GRAD><<<grid, dim3(256), 0, st>>>(t);
   else distill_stream_kernel<T, 512, TWO, GRAD><<<grid, dim3(512), 0, st>>>(t);
 }
 
 template <typename T, bool TWO, bool GRAD> hipError_t launch(const DistillArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.n * a.T;
   const DistillPlan plan = plan_distill(rows, a.V, a.K, a.type);
-  const int32_t packs = a.V / kVec<T>;
-  const uint32_t blocks = (uint32_t)std::min(rows, kMostRowBlocks);
-  // (the loss alone, of rows of more than 256 packs)
-  if (plan.parts > 1 || packs > 1024 * 16 || (!GRAD && packs > 256)) {
+  const DistillTile tile = tile_of(plan, a.V, a.type, GRAD);
+  if (tile.packs == 0) {
     StreamArgs t{a, rows, plan.parts, plan.cols, STREAM_ALL, nullptr, nullptr};
     if (plan.parts > 1) {
       t.stats = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.stats);
       t.values = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + plan.values);
       t.mode = STREAM_STATS;
-      stream<T, TWO, false>(t, st);
+      stream<T, TWO, false>(t, tile.threads, st);
       t.mode = STREAM_REST;
     }
-    stream<T, TWO, GRAD>(t, st);
+    stream<T, TWO, GRAD>(t, tile.threads, st);
     return hipGetLastError();
   }
-  // As many threads as the row needs with 12 or 16 packs each.  Rows of up to 512 threads leave room for several workgroups on a compute
-  // unit, of which some load while others compute: one row each (7936 rows of 32000 bf16, two softmaxes 201 us; looping, with the
-  // next row's loads in between, 242).  Rows of 1024 threads have the compute unit to themselves and loop (15872 rows of
-  // 128000 bf16 1507 us, 5.1 TB/s; with the loads between the rows it took 230 us more).
-  if (packs <= 64) distill_row_kernel<T, 64, 1, TWO, GRAD, false><<<blocks, dim3(64), 0, st>>>(a, rows);
-  else if (packs <= 64 * 4) distill_row_kernel<T, 64, 4, TWO, GRAD, false><<<blocks, dim3(64), 0, st>>>(a, rows);
+  const dim3 grid((uint32_t)std::min(rows, tile.loop ? (int64_t)256 : kMostRowBlocks)), block(tile.threads);
+  const int32_t at_most = tile.threads * tile.packs;
+  if (at_most == 64 * 1) distill_row_kernel<T, 64, 1, TWO, GRAD, false><<<grid, block, 0, st>>>(a, rows);
+  else if (at_most == 64 * 4) distill_row_kernel<T, 64, 4, TWO, GRAD, false><<<grid, block, 0, st>>>(a, rows);
   else if constexpr (GRAD) {
-    if (packs <= 256 * 4) distill_row_kernel<T, 256, 4, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
-    else if (packs <= 256 * 8) distill_row_kernel<T, 256, 8, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
-    else if (packs <= 256 * 12) distill_row_kernel<T, 256, 12, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
-    else if (packs <= 256 * 16) distill_row_kernel<T, 256, 16, TWO, true, false><<<blocks, dim3(256), 0, st>>>(a, rows);
-    else if (packs <= 512 * 12) distill_row_kernel<T, 512, 12, TWO, true, false><<<blocks, dim3(512), 0, st>>>(a, rows);
-    else if (packs <= 512 * 16) distill_row_kernel<T, 512, 16, TWO, true, false><<<blocks, dim3(512), 0, st>>>(a, rows);
-    else if (packs <= 1024 * 12) distill_row_kernel<T, 1024, 12, TWO, true, true><<<dim3((uint32_t)std::min<int64_t>(rows, 256)), dim3(1024), 0, st>>>(a, rows);
-    else distill_row_kernel<T, 1024, 16, TWO, true, true><<<dim3((uint32_t)std::min<int64_t>(rows, 256)), dim3(1024), 0, st>>>(a, rows);
+    if (at_most == 256 * 4) distill_row_kernel<T, 256, 4, TWO, true, false><<<grid, block, 0, st>>>(a, rows);
+    else if (at_most == 256 * 8) distill_row_kernel<T, 256, 8, TWO, true, false><<<grid, block, 0, st>>>(a, rows);
+    else if (at_most == 256 * 12) distill_row_kernel<T, 256, 12, TWO, true, false><<<grid, block, 0, st>>>(a, rows);
+    else if (at_most == 256 * 16) distill_row_kernel<T, 256, 16, TWO, true, false><<<grid, block, 0, st>>>(a, rows);
+    else if (at_most == 512 * 12) distill_row_kernel<T, 512, 12, TWO, true, false><<<grid, block, 0, st>>>(a, rows);
+    else if (at_most == 512 * 16) distill_row_kernel<T, 512, 16, TWO, true, false><<<grid, block, 0, st>>>(a, rows);
+    else if (at_most == 1024 * 12) distill_row_kernel<T, 1024, 12, TWO, true, true><<<grid, block, 0, st>>>(a, rows);
+    else distill_row_kernel<T, 1024, 16, TWO, true, true><<<grid, block, 0, st>>>(a, rows);
   }
   return hipGetLastError();
 }
@@ -653,6 +667,15 @@ DistillPlan plan_distill(int64_t rows, int32_t V, int32_t K, int type) {
     p.bytes = p.values + (rows * (K + 1) * 4 + 255) / 256 * 256;
   }
   return p;
+}
+
+void describe_distill(int64_t rows, int32_t V, int32_t K, int type, bool grad, int32_t* out) {
+  const DistillPlan plan = plan_distill(rows, V, K, type);
+  const DistillTile tile = tile_of(plan, V, type, grad);
+  out[0] = tile.threads;
+  out[1] = tile.packs;
+  out[2] = tile.loop;
+  out[3] = plan.parts;
 }
 
 hipError_t launch_distill(const DistillArgs& a, hipStream_t st) {

@@ -500,20 +500,28 @@ constexpr int64_t kMostBlocks = 1 << 20, kMostZeros = 15 << 20;    // a launch h
 int32_t run_of(const EmbedArgs& a, int64_t floats) { return (int32_t)std::max<int64_t>(std::min<int64_t>(floats / a.h, a.V), 1); }
 uint32_t four_a_block(int64_t units) { return (uint32_t)std::min((units + 3) / 4, kMostBlocks); }
 
+// Columns a lane takes: short rows keep enough lanes with columns of their own.
+int32_t columns_of(int32_t h) { return h > 128 ? 4 : h > 64 ? 2 : 1; }
+int32_t tiles_of(int32_t h, int32_t vec) { return (h + 64 * vec - 1) / (64 * vec); }
+// Four positions a wavefront once there are wavefronts enough (31 x 2048 positions of 512 bf16: 31.2 us, with two 33.5, eight 33.6).
+int32_t positions_of(int64_t rows, int32_t tiles) { return rows * tiles >= 1 << 14 ? 4 : 1; }
+
 template <typename T, int VEC> hipError_t lookup(const EmbedArgs& a, hipStream_t st) {
-  const int32_t tiles = (a.h + 64 * VEC - 1) / (64 * VEC);
+  const int32_t tiles = tiles_of(a.h, VEC);
   const int64_t rows = (int64_t)a.n * a.T;
-  // four positions a wavefront once there are wavefronts enough (31 x 2048 positions of 512 bf16: 31.2 us, with two 33.5, eight 33.6)
-  if (rows * tiles >= 1 << 14) embed_kernel<T, VEC, 4><<<dim3(four_a_block((rows + 3) / 4 * tiles)), dim3(256), 0, st>>>(a, tiles);
+  if (positions_of(rows, tiles) == 4) embed_kernel<T, VEC, 4><<<dim3(four_a_block((rows + 3) / 4 * tiles)), dim3(256), 0, st>>>(a, tiles);
   else embed_kernel<T, VEC, 1><<<dim3(four_a_block(rows * tiles)), dim3(256), 0, st>>>(a, tiles);
   return hipGetLastError();
 }
 template <typename T> struct Lookup {
-  static hipError_t go(const EmbedArgs& a, hipStream_t st) { return a.h > 128 ? lookup<T, 4>(a, st) : a.h > 64 ? lookup<T, 2>(a, st) : lookup<T, 1>(a, st); }
+  static hipError_t go(const EmbedArgs& a, hipStream_t st) {
+    const int32_t vec = columns_of(a.h);
+    return vec == 4 ? lookup<T, 4>(a, st) : vec == 2 ? lookup<T, 2>(a, st) : lookup<T, 1>(a, st);
+  }
 };
 
 template <typename T, int VEC, int NT> hipError_t few_positions(const EmbedArgs& a, hipStream_t st) {
-  const int32_t tiles = (a.h + 64 * VEC - 1) / (64 * VEC), run = run_of(a, 1024);
+  const int32_t tiles = tiles_of(a.h, VEC), run = run_of(a, 1024);
   const int64_t runs = (a.V + (int64_t)run - 1) / run;
   const int64_t units = (int64_t)a.n * a.T * tiles + (a.accumulate ? 0 : a.n * runs);
   if (units == 0) return hipSuccess;
@@ -535,8 +543,11 @@ constexpr int64_t kFewZeros = 16 << 20;
 bool zeros_ride(const EmbedArgs& a) {
   return a.ldr == a.h && (int64_t)a.n * a.V * a.h <= kFewZeros && zero_args(a, 4096).all <= 1u << 16;
 }
-hipError_t zeros(const EmbedArgs& a, hipStream_t st) {
-  if (a.ldr != a.h) {
+// Who writes the zeros of sorted positions' tables.
+enum ZeroForm : int { ZEROS_NONE = 0, ZEROS_WITH_SORT = 1, ZEROS_ALONE = 2, ZEROS_BY_ROW = 3 };
+ZeroForm zero_form(const EmbedArgs& a) { return a.accumulate ? ZEROS_NONE : zeros_ride(a) ? ZEROS_WITH_SORT : a.ldr == a.h ? ZEROS_ALONE : ZEROS_BY_ROW; }
+hipError_t zeros(const EmbedArgs& a, ZeroForm form, hipStream_t st) {
+  if (form == ZEROS_BY_ROW) {
     zero_rows_kernel<<<dim3(four_a_block((int64_t)a.n * a.V)), dim3(256), 0, st>>>(a);
     return hipGetLastError();
   }
@@ -544,6 +555,10 @@ hipError_t zeros(const EmbedArgs& a, hipStream_t st) {
   zeros_kernel<<<dim3((uint32_t)std::min<int64_t>(z.all, kMostZeros)), dim3(256), 0, st>>>(z);
   return hipGetLastError();
 }
+
+// Tokens a lane holds of positions that are not sorted, and positions a thread has of those that one workgroup sorts.
+int32_t few_of(int64_t T) { return T <= 64 ? 1 : T <= 256 ? 4 : 16; }
+int32_t keys_of(int64_t T) { return T <= 1024 ? 1 : T <= 2048 ? 2 : T <= 4096 ? 4 : 8; }
 
 template <int IPT> hipError_t sort_lds(const EmbedArgs& a, const EmbedGradPlan& p, const ZeroArgs& z, hipStream_t st) {
   const size_t lds = (16 * kDigits + 16 + IPT * 1024) * sizeof(uint32_t);
@@ -557,16 +572,20 @@ template <int IPT> hipError_t sort_lds(const EmbedArgs& a, const EmbedGradPlan& 
 }
 
 template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const EmbedGradPlan& p, hipStream_t st) {
-  if (p.small) return a.T <= 64 ? few_positions<T, VEC, 1>(a, st) : a.T <= 256 ? few_positions<T, VEC, 4>(a, st) : few_positions<T, VEC, 16>(a, st);
+  if (p.small) {
+    const int32_t few = few_of(a.T);
+    return few == 1 ? few_positions<T, VEC, 1>(a, st) : few == 4 ? few_positions<T, VEC, 4>(a, st) : few_positions<T, VEC, 16>(a, st);
+  }
   char* ws = static_cast<char*>(a.workspace);
   auto words = [&](int64_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
   uint32_t *tok = words(p.tok0), *pos = words(p.pos0);
-  const bool ride = !a.accumulate && zeros_ride(a);
-  const ZeroArgs z = ride ? zero_args(a, 4096) : ZeroArgs{};
-  hipError_t e = a.accumulate || ride ? hipSuccess : zeros(a, st);
+  const ZeroForm form = zero_form(a);
+  const ZeroArgs z = form == ZEROS_WITH_SORT ? zero_args(a, 4096) : ZeroArgs{};
+  hipError_t e = form == ZEROS_ALONE || form == ZEROS_BY_ROW ? zeros(a, form, st) : hipSuccess;
   if (e != hipSuccess) return e;
   if (p.lds) {
-    e = a.T <= 1024 ? sort_lds<1>(a, p, z, st) : a.T <= 2048 ? sort_lds<2>(a, p, z, st) : a.T <= 4096 ? sort_lds<4>(a, p, z, st) : sort_lds<8>(a, p, z, st);
+    const int32_t keys = keys_of(a.T);
+    e = keys == 1 ? sort_lds<1>(a, p, z, st) : keys == 2 ? sort_lds<2>(a, p, z, st) : keys == 4 ? sort_lds<4>(a, p, z, st) : sort_lds<8>(a, p, z, st);
   } else {
     uint32_t *tok2 = words(p.tok1), *pos2 = words(p.pos1);
     const dim3 grid((uint32_t)std::min((int64_t)a.n * p.tiles, kMostBlocks));
@@ -588,7 +607,7 @@ template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const Emb
     }
   }
   if (e != hipSuccess) return e;
-  WalkArgs w{a, tok, pos, reinterpret_cast<float*>(ws + p.partial), p.pitch, p.chunks, (a.h + 64 * VEC - 1) / (64 * VEC)};
+  WalkArgs w{a, tok, pos, reinterpret_cast<float*>(ws + p.partial), p.pitch, p.chunks, tiles_of(a.h, VEC)};
   const dim3 walk(four_a_block((int64_t)a.n * p.chunks * w.tiles)), join(four_a_block((int64_t)a.n * (p.chunks - 1) * w.tiles));
   if (a.accumulate) {
     walk_kernel<T, VEC, true><<<walk, dim3(256), 0, st>>>(w);
@@ -603,8 +622,8 @@ template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const Emb
 template <typename T> struct Gradient {
   static hipError_t go(const EmbedArgs& a, hipStream_t st) {
     const EmbedGradPlan p = plan_embed_grad(a.n, a.V, a.h, a.T);
-    // short rows: enough lanes with columns of their own
-    return a.h > 128 ? gradient<T, 4>(a, p, st) : a.h > 64 ? gradient<T, 2>(a, p, st) : gradient<T, 1>(a, p, st);
+    const int32_t vec = columns_of(a.h);
+    return vec == 4 ? gradient<T, 4>(a, p, st) : vec == 2 ? gradient<T, 2>(a, p, st) : gradient<T, 1>(a, p, st);
   }
 };
 
@@ -615,6 +634,19 @@ template <template <typename> class Launch, typename... A> hipError_t by_type(in
 }
 
 }  // namespace
+
+void describe_embed(const EmbedArgs& a, int32_t* out) {
+  out[0] = columns_of(a.h);
+  out[1] = positions_of((int64_t)a.n * a.T, tiles_of(a.h, out[0]));
+}
+void describe_embed_grad(const EmbedArgs& a, int32_t* out) {
+  const EmbedGradPlan p = plan_embed_grad(a.n, a.V, a.h, a.T);
+  out[0] = columns_of(a.h);
+  out[1] = p.small ? few_of(a.T) : 0;
+  out[2] = !p.small && p.lds ? keys_of(a.T) : 0;
+  out[3] = !p.small && !p.lds ? tile_of_sort(a.T) : 0;
+  out[4] = p.small ? ZEROS_NONE : zero_form(a);
+}
 
 hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) { return by_type<Lookup>(a.type, a, st); }
 hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st) { return by_type<Gradient>(a.type, a, st); }

@@ -110,6 +110,12 @@ TopPlan plan_top(int64_t rows, int32_t V, int32_t K, int type);
 
 constexpr int kTopMax = 256;         // most entries of a row's top logits
 
+// What a call of these sizes launches (ceca_describe_text_launch): the pointers of `a` are not looked at.
+void describe_embed(const EmbedArgs& a, int32_t* out);
+void describe_embed_grad(const EmbedArgs& a, int32_t* out);
+void describe_distill(int64_t rows, int32_t V, int32_t K, int type, bool grad, int32_t* out);
+void describe_top(int64_t rows, int32_t V, int32_t K, int type, int32_t* out);
+
 hipError_t launch_embed(const EmbedArgs& a, hipStream_t st);
 hipError_t launch_embed_grad(const EmbedArgs& a, hipStream_t st);
 hipError_t launch_distill(const DistillArgs& a, hipStream_t st);

@@ -357,25 +357,44 @@ __global__ __launch_bounds__(kMergeThreads) void top_merge_kernel(MergeArgs m) {
 
 constexpr int64_t kMostTopBlocks = 1 << 22;
 
-template <typename T> hipError_t launch(const TopArgs& a, hipStream_t st) {
-  const TopPlan plan = plan_top(a.rows, a.V, a.K, a.type);
-  const int32_t packs = plan.cols / kVec<T>;
+// A workgroup's threads and the packs that each holds.
+struct TopTile { int32_t threads, packs; };
+TopTile tile_of(const TopPlan& plan, int64_t rows, int type) {
+  const int32_t packs = plan.cols / (type == TYPE_F32 ? 4 : 8);
   // 256 threads with up to 16 packs each: several rows on a compute unit, of which some load while others look for their threshold
   // (7936 rows of 32000 bf16, K = 64: 120 us; 512 threads with 8 packs 140, 128 with 32 212, 1024 with 4 376).  Longer rows
   // in parts: 1000 rows of 33216 fp32, K = 157, 67 us, in one tile of 512 threads 89.  Many short rows by a wavefront each, which
   // needs no barriers (87219 rows of 2304 bf16, K = 6: 143 us, by 256 threads 313); few of them are done sooner by more threads.
-  const dim3 grid((uint32_t)std::min((int64_t)a.rows * plan.parts, kMostTopBlocks));
-  if (packs <= 64) top_kernel<T, 64, 1><<<grid, dim3(64), 0, st>>>(a, plan);
-  else if (packs <= 64 * 4) top_kernel<T, 64, 4><<<grid, dim3(64), 0, st>>>(a, plan);
-  else if (packs <= 256 * 4 && grid.x <= 2048) top_kernel<T, 256, 4><<<grid, dim3(256), 0, st>>>(a, plan);
-  else if (packs <= 64 * 8) top_kernel<T, 64, 8><<<grid, dim3(64), 0, st>>>(a, plan);
-  else if (packs <= 64 * 16) top_kernel<T, 64, 16><<<grid, dim3(64), 0, st>>>(a, plan);
-  else if (packs <= 256 * 8) top_kernel<T, 256, 8><<<grid, dim3(256), 0, st>>>(a, plan);
-  else top_kernel<T, 256, 16><<<grid, dim3(256), 0, st>>>(a, plan);
+  if (packs <= 64) return {64, 1};
+  if (packs <= 64 * 4) return {64, 4};
+  if (packs <= 256 * 4 && rows * plan.parts <= 2048) return {256, 4};
+  if (packs <= 64 * 8) return {64, 8};
+  if (packs <= 64 * 16) return {64, 16};
+  return {256, packs <= 256 * 8 ? 8 : 16};
+}
+MergeArgs merge_of(const TopArgs& a, const uint64_t* in, uint64_t* out, int32_t lists) {
+  MergeArgs m{a, in, out, lists, kMergeWords / a.K, 0};
+  m.groups = (lists + m.per - 1) / m.per;
+  return m;
+}
+
+template <typename T> hipError_t launch(const TopArgs& a, hipStream_t st) {
+  const TopPlan plan = plan_top(a.rows, a.V, a.K, a.type);
+  const TopTile tile = tile_of(plan, a.rows, a.type);
+  const dim3 grid((uint32_t)std::min((int64_t)a.rows * plan.parts, kMostTopBlocks)), block(tile.threads);
+  if (tile.threads == 64) {
+    if (tile.packs == 1) top_kernel<T, 64, 1><<<grid, block, 0, st>>>(a, plan);
+    else if (tile.packs == 4) top_kernel<T, 64, 4><<<grid, block, 0, st>>>(a, plan);
+    else if (tile.packs == 8) top_kernel<T, 64, 8><<<grid, block, 0, st>>>(a, plan);
+    else top_kernel<T, 64, 16><<<grid, block, 0, st>>>(a, plan);
+  } else {
+    if (tile.packs == 4) top_kernel<T, 256, 4><<<grid, block, 0, st>>>(a, plan);
+    else if (tile.packs == 8) top_kernel<T, 256, 8><<<grid, block, 0, st>>>(a, plan);
+    else top_kernel<T, 256, 16><<<grid, block, 0, st>>>(a, plan);
+  }
   uint64_t *in = static_cast<uint64_t*>(a.workspace), *out = in + plan.second / 8;
   for (int32_t lists = plan.parts; lists > 1;) {
-    MergeArgs m{a, in, out, lists, kMergeWords / a.K, 0};
-    m.groups = (lists + m.per - 1) / m.per;
+    MergeArgs m = merge_of(a, in, out, lists);
     if (m.groups == 1) m.out = nullptr;
     top_merge_kernel<T><<<dim3((uint32_t)std::min((int64_t)a.rows * m.groups, kMostTopBlocks)), dim3(kMergeThreads), 0, st>>>(m);
     lists = m.groups;
@@ -402,6 +421,18 @@ TopPlan plan_top(int64_t rows, int32_t V, int32_t K, int type) {
     p.bytes = p.second + (groups > 1 ? (rows * groups * K * 8 + 255) / 256 * 256 : 0);
   }
   return p;
+}
+
+void describe_top(int64_t rows, int32_t V, int32_t K, int type, int32_t* out) {
+  const TopPlan plan = plan_top(rows, V, K, type);
+  const TopTile tile = tile_of(plan, rows, type);
+  TopArgs a{};
+  a.K = K;
+  out[0] = tile.threads;
+  out[1] = tile.packs;
+  out[2] = plan.parts;
+  out[3] = 0;
+  for (int32_t lists = plan.parts; lists > 1; lists = merge_of(a, nullptr, nullptr, lists).groups) ++out[3];
 }
 
 hipError_t launch_top(const TopArgs& a, hipStream_t st) {
