@@ -98,12 +98,12 @@ int32_t ceca_describe_step_launch(int32_t n, int64_t d, int64_t ld, int32_t r, i
                                   int32_t in_place, int32_t* out);
 
 /* The kernels that a call of a language-model operator launches, so that a test that means one of them can ask whether its
- * sizes reach it.  Nothing is launched.  n agents with T positions each; type: of the activations or logits; out: host, 5 int32
+ * sizes reach it.  Nothing is launched.  n agents with T positions each; type: of the activations or logits; out: host, 6 int32
  * (0 where not named below):
  *   CECA_TEXT_EMBED    ceca_embed, width = h: columns per lane, positions per wavefront
  *   CECA_TEXT_GRAD     ceca_embed_grad, width = h: columns per lane; tokens per lane where nothing is sorted; positions per thread where one
  *                      workgroup sorts an agent's; positions per workgroup where several do; who writes the zeros (1 the sort's launch,
- *                      2 a launch over whole pieces, 3 one over rows)
+ *                      2 a launch over whole pieces, 3 one over rows); whether a launch sums up the workgroups' counts
  *   CECA_TEXT_DISTILL  ceca_distill, width = K: threads per workgroup, packs of 16 bytes per thread (0: rows stream), whether workgroups loop
  *                      over rows, parts of a row
  *   CECA_TEXT_TOP      ceca_top_logits with n T rows, width = K: threads per workgroup, packs per thread, parts of a row, merging launches

@@ -475,8 +475,8 @@ def ceca_describe_step_launch(n: int, d: int, ld: int, r: int, port: int, kind: 
 
 
 def ceca_describe_text_launch(call: int, type: int, n: int, T: int, V: int, width: int, flags: int = 0) -> tuple:
-    """The kernels that a language-model operator's call of these sizes launches (ceca_test.h says what the five numbers are)."""
-    out = (C.c_int32 * 5)()
+    """The kernels that a language-model operator's call of these sizes launches (ceca_test.h says what the six numbers are)."""
+    out = (C.c_int32 * 6)()
     _check(lib().ceca_describe_text_launch(call, type, n, T, V, width, flags, out))
     return tuple(out)
 

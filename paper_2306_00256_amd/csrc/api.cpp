@@ -1510,7 +1510,7 @@ int32_t ceca_top_logits(const void* logits, int32_t type, int64_t ld, int32_t ro
 int32_t ceca_describe_text_launch(int32_t call, int32_t type, int32_t n, int32_t T, int32_t V, int32_t width, int32_t flags, int32_t* out) {
   if (!out) return fail(CECA_EINVAL, "null pointer");
   if (call < CECA_TEXT_EMBED || call > CECA_TEXT_TOP || flags < 0 || flags > 15) return fail(CECA_EINVAL, "unknown call %d or flags %d", call, flags);
-  for (int k = 0; k < 5; ++k) out[k] = 0;
+  for (int k = 0; k < 6; ++k) out[k] = 0;
   if (call <= CECA_TEXT_GRAD) {
     // stand-in addresses (never dereferenced), far apart
     void* const at[] = {reinterpret_cast<void*>(uintptr_t(1) << 50), reinterpret_cast<void*>(uintptr_t(1) << 52), reinterpret_cast<void*>(uintptr_t(1) << 54)};

@@ -206,7 +206,7 @@ struct PassArgs {
   const int32_t* tokens;       // first pass, else null
   const uint32_t *tok, *pos;   // later passes
   uint32_t *tok_out, *pos_out, *hist;
-  int32_t n, V, T, tiles, shift, bits;
+  int32_t n, V, T, tiles, hist_rows, shift, bits;
 };
 __device__ __forceinline__ uint32_t pass_key(const PassArgs& p, int64_t i, int64_t t) {
   if (!p.tokens) return p.tok[i * p.T + t];
@@ -222,14 +222,35 @@ template <int IPT> __global__ __launch_bounds__(1024) void count_digits_kernel(P
   __shared__ uint32_t count[kDigits];
   const int64_t sorts = (int64_t)p.n * p.tiles;
   for (int64_t b = blockIdx.x; b < sorts; b += counts) {
-    const int64_t i = b / p.tiles, t0 = (b - i * p.tiles) * kTile;
+    const int64_t i = b / p.tiles, tile = b - i * p.tiles, t0 = tile * kTile;
     if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
     __syncthreads();
     for (int64_t t = t0 + threadIdx.x; t < min(t0 + kTile, (int64_t)p.T); t += 1024)
       atomicAdd(&count[pass_key(p, i, t) >> p.shift & ((1u << p.bits) - 1)], 1u);       // whole numbers: any order
     __syncthreads();
-    if (threadIdx.x < kDigits) p.hist[b * kDigits + threadIdx.x] = count[threadIdx.x];
+    if (threadIdx.x < kDigits) p.hist[(i * p.hist_rows + tile) * kDigits + threadIdx.x] = count[threadIdx.x];
     __syncthreads();
+  }
+}
+// ... then, of many tiles, a digit's counts of earlier tiles and of all, by a wavefront per agent and digit ...
+__global__ __launch_bounds__(256) void sum_counts_kernel(PassArgs p) {
+  const int lane = threadIdx.x % 64;
+  const int64_t units = (int64_t)p.n * kDigits;
+  for (int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; unit < units; unit += (int64_t)gridDim.x * 4) {
+    uint32_t* hist = p.hist + unit / kDigits * p.hist_rows * kDigits + unit % kDigits;
+    uint32_t before = 0;
+    for (int64_t k0 = 0; k0 < p.tiles; k0 += 64) {
+      const uint32_t mine = k0 + lane < p.tiles ? hist[(k0 + lane) * kDigits] : 0;
+      uint32_t upto = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t x = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += x;
+      }
+      if (k0 + lane < p.tiles) hist[(k0 + lane) * kDigits] = before + upto - mine;
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (lane == 0) hist[(int64_t)p.tiles * kDigits] = before;
   }
 }
 // ... then every tile's keys to their places: behind the smaller digits of all tiles and the same digit's of earlier tiles.
@@ -243,11 +264,17 @@ template <int IPT> __global__ __launch_bounds__(1024) void place_keys_kernel(Pas
     const int32_t tile = (int32_t)(b - i * p.tiles);
     uint32_t before = 0, all = 0;
     if (tid < kDigits) {
+      const uint32_t* hist = p.hist + i * p.hist_rows * kDigits + tid;
+      if (p.hist_rows > p.tiles) {
+        before = hist[(int64_t)tile * kDigits];
+        all = hist[(int64_t)p.tiles * kDigits];
+      } else {
 #pragma unroll 8
-      for (int32_t k = 0; k < p.tiles; ++k) {
-        const uint32_t c = p.hist[(i * p.tiles + k) * kDigits + tid];
-        all += c;
-        before += k < tile ? c : 0;
+        for (int32_t k = 0; k < p.tiles; ++k) {
+          const uint32_t c = hist[k * kDigits];
+          all += c;
+          before += k < tile ? c : 0;
+        }
       }
     }
     uint32_t upto = all;
@@ -590,7 +617,7 @@ template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const Emb
     uint32_t *tok2 = words(p.tok1), *pos2 = words(p.pos1);
     const dim3 grid((uint32_t)std::min((int64_t)a.n * p.tiles, kMostBlocks));
     for (int k = 0; k < p.passes && e == hipSuccess; ++k) {
-      const PassArgs q{k ? nullptr : a.tokens, tok, pos, tok2, pos2, words(p.hist), a.n, a.V, a.T, p.tiles, k * p.digit_bits,
+      const PassArgs q{k ? nullptr : a.tokens, tok, pos, tok2, pos2, words(p.hist), a.n, a.V, a.T, p.tiles, p.hist_rows, k * p.digit_bits,
                        std::min(p.digit_bits, p.bits - k * p.digit_bits)};
       const ZeroArgs zk = k ? ZeroArgs{} : z;
       const dim3 counts(grid.x + zk.all);
@@ -599,6 +626,7 @@ template <typename T, int VEC> hipError_t gradient(const EmbedArgs& a, const Emb
         place_keys_kernel<1><<<grid, dim3(1024), 0, st>>>(q);
       } else {
         count_digits_kernel<4><<<counts, dim3(1024), 0, st>>>(q, zk, grid.x);
+        if (q.hist_rows > q.tiles) sum_counts_kernel<<<dim3(four_a_block((int64_t)a.n * kDigits)), dim3(256), 0, st>>>(q);
         place_keys_kernel<4><<<grid, dim3(1024), 0, st>>>(q);
       }
       e = hipGetLastError();
@@ -646,6 +674,7 @@ void describe_embed_grad(const EmbedArgs& a, int32_t* out) {
   out[2] = !p.small && p.lds ? keys_of(a.T) : 0;
   out[3] = !p.small && !p.lds ? tile_of_sort(a.T) : 0;
   out[4] = p.small ? ZEROS_NONE : zero_form(a);
+  out[5] = !p.small && p.hist_rows > p.tiles;
 }
 
 hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) { return by_type<Lookup>(a.type, a, st); }

@@ -32,9 +32,14 @@ constexpr int64_t kSomePositions = 4096;
 // Positions per workgroup where several sort together: 1024, one a thread, while few workgroups have to add up the others' counts.
 constexpr int tile_of_sort(int64_t T) { return T <= (1 << 16) ? 1024 : 4096; }
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+// Up to this many tiles every one adds up the others' counts itself; beyond, a launch of its own does it for all, or the work would grow with
+// the square of T (positions of 2 fp16, V = 32000: 2^18 of them, 65 tiles, 88.7 us either way; 2^20 292 -> 254; 2^25 32.5 -> 7.7 ms).
+constexpr int kManyTiles = 64;
+static_assert((1 << 16) / 1024 <= kManyTiles, "tiles of 1024 positions are not many");
 struct EmbedGradPlan {
   bool small, lds;
   int32_t bits, pos_bits, chunks, tiles;
+  int32_t hist_rows;                   // counts of an agent: one row per tile and, where a launch of its own sums them up, one for all
   int32_t passes, digit_bits;          // of the sort
   int64_t pitch;                       // floats per partial sum
   int64_t tok0, pos0, tok1, pos1, hist, partial, bytes;   // offsets in the workspace
@@ -59,7 +64,8 @@ inline EmbedGradPlan plan_embed_grad(int64_t n, int64_t V, int64_t h, int64_t T)
   if (!p.lds) {
     p.tok1 = take(n * T * 4);
     p.pos1 = take(n * T * 4);
-    p.hist = take(n * p.tiles * (int64_t)kDigits * 4);
+    p.hist_rows = p.tiles + (p.tiles > kManyTiles);
+    p.hist = take(n * p.hist_rows * (int64_t)kDigits * 4);
   }
   p.partial = take(n * p.chunks * 2 * p.pitch * 4);
   return p;

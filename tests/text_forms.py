@@ -12,6 +12,7 @@ LOOKUPS = [(d, n, T, h) for d in CODE for h in (40, 100, 300) for n, T in ((3, 5
 GRADIENTS = [(d, 2, T, 70, h, acc, 0, 0) for d in CODE for h in (40, 100, 300) for T in (50, 200, 900) for acc in (False, True)]       # not sorted
 GRADIENTS += [(d, 3, 1500, 333, h, acc, 0, 0) for d in CODE for h in (40, 100, 300) for acc in (False, True)]
 GRADIENTS += [("bfloat16", n, T, 2500, 100, acc, 0, 0) for n, T in ((6, 1000), (2, 1900), (2, 3900), (2, 7900), (2, 9000), (1, 70000)) for acc in (False, True)]
+GRADIENTS += [(d, 2, 270_000, 2500, 3, acc, 0, 0) for d in ("float32", "bfloat16") for acc in (False, True)]
 # zeros beside the sort and on their own (over 2^24 floats), in one piece and table by table, and row by row
 GRADIENTS += [("bfloat16", 3, T, 2001, 36, False, 5, 0) for T in (1500, 9000)]
 GRADIENTS += [("float16", 2, T, 70001, 130, False, apart, 0) for T in (1500, 9000) for apart in (0, 3)]
@@ -35,22 +36,22 @@ def lookup_keys(case):
 def gradient_keys(case):
     d, n, T, V, h, acc, apart, pitch = case
     flags = (B.TEXT_ACCUMULATE if acc else 0) | (B.TEXT_APART if apart else 0) | (B.TEXT_PITCH if pitch else 0)
-    vec, few, keys, tile, zeros = B.ceca_describe_text_launch(B.TEXT_GRAD, CODE[d], n, T, V, h, flags)
+    vec, few, keys, tile, zeros, sums = B.ceca_describe_text_launch(B.TEXT_GRAD, CODE[d], n, T, V, h, flags)
     if few:
         return {("few", d, vec, few, acc)}
-    return {("walk", d, vec, acc), ("join", vec, acc), ("sort", keys, tile), ("pitch", bool(pitch), acc)} | ({("zeros", zeros, keys > 0, bool(apart) and zeros < 3)} if not acc else set())
+    return {("walk", d, vec, acc), ("join", vec, acc), ("sort", keys, tile, sums), ("pitch", bool(pitch), acc)} | ({("zeros", zeros, keys > 0, bool(apart) and zeros < 3)} if not acc else set())
 
 
 def distillation_keys(case):
     d, rows, V = case
     out = set()
     for flag in (0, B.TEXT_WITH_GRAD):
-        threads, packs, loop, parts, _ = B.ceca_describe_text_launch(B.TEXT_DISTILL, CODE[d], 1, rows, V, 8, flag)
+        threads, packs, loop, parts = B.ceca_describe_text_launch(B.TEXT_DISTILL, CODE[d], 1, rows, V, 8, flag)[:4]
         out.add(("distill", d, threads, packs, loop, parts > 1, bool(flag)))
     return out
 
 
 def top_keys(case):
     d, rows, V, K = case
-    threads, packs, parts, merges, _ = B.ceca_describe_text_launch(B.TEXT_TOP, CODE[d], 1, rows, V, K, 0)
+    threads, packs, parts, merges = B.ceca_describe_text_launch(B.TEXT_TOP, CODE[d], 1, rows, V, K, 0)[:4]
     return {("top", d, threads, packs), ("merge", d, min(merges, 2))}
