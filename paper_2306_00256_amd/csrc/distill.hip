@@ -654,7 +654,9 @@ DistillPlan plan_distill(int64_t rows, int32_t V, int32_t K, int type) {
   p.parts = 1;
   p.cols = V;
   const int32_t vec = type == TYPE_F32 ? 4 : 8;
-  // few rows of many columns, or not very many of more than registers hold: 4096 columns a part or more, up to 512 workgroups
+  // few rows of many columns, or not very many of more than registers hold: 4096 columns a part or more, up to 512 workgroups (with gradient, in
+  // parts against whole: 65 rows of 128000 bf16 16 us against 26, 128 21 against 27, 192 34 against 28; but 100 rows of 65536 16 against 12.6, of 40000
+  // fp32 14.6 against 13.2, and the losses alone 12.3 against 9.0 and 11.5 against 7.5)
   if (rows > 0 && ((rows <= 64 && V >= 32768) || (rows <= 256 && V / vec > 1024 * 16))) {
     const int32_t most = (int32_t)std::min<int64_t>(V / 4096, (512 + rows - 1) / rows);
     if (most > 1) {
