@@ -321,7 +321,8 @@ int32_t ceca_graph_rounds(const float* X_in, float* X_out, int32_t n, int64_t d,
  * computed in fp32 and rounded once, to nearest even, where a result is stored in 16 bits.  The results of a call depend on
  * its arguments alone: no floating-point atomics are used.  Pointers lie on their element type's boundary (CECA_EINVAL
  * otherwise); pitches are counted in elements.  n T, the number of positions, is below 2^31; T = 0 does nothing (and
- * ceca_embed_grad then sees no token).  A workspace serves one call at a time: calls that may overlap (other streams, graphs that
+ * ceca_embed_grad then sees no token).  Buffers are disjoint where their spans, from the first to the last element, are: rows of one
+ * that lie between rows of another are refused.  A workspace serves one call at a time: calls that may overlap (other streams, graphs that
  * are replayed side by side) need one each. */
 enum { CECA_F32 = 0, CECA_BF16 = 1, CECA_F16 = 2 };
 
@@ -365,7 +366,7 @@ int32_t ceca_embed_grad(const void* G, int32_t type, int64_t ldg, const int32_t*
  *     and entries are not looked at (padding may hold anything).
  *   - Exponentials are taken of differences from the row's largest value: with x such a difference over the temperature, a share is
  *     off by up to (4 |x| + V / 64 + 64) 2^-24 of itself, and one below 2^-126 of the largest is zero (an entry so small has no part in loss
- *     and gradient, masked or not).
+ *     and gradient, masked or not); a difference beyond fp32's range is infinite.
  *   - Otherwise a NaN or +inf among a row's logits makes its loss and its whole gradient NaN; one among its entries' values its soft
  *     loss and the gradient at its entries' places. */
 #define CECA_TOP_MAX 256
